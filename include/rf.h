@@ -282,6 +282,107 @@ RF_API rf_status rf_rmsnorm_gemm_ws(const rf_tensor* x, const rf_tensor* g, cons
                           rf_tensor* y, float eps, void* workspace, size_t workspace_bytes,
                           rf_stream stream);
 
+/*
+ * ---- a serving step: packed sequences over a paged cache ----
+ *
+ * The new tokens of B sequences are packed one behind the other: [T, heads, d] tensors in which sequence b owns the
+ * rows seq_start[b] .. seq_start[b+1]-1 (0 <= seq_start[0] <= .. <= seq_start[B] <= T; a sequence may have none, and
+ * rows behind the last sequence are neither read nor written).  Their keys and values live in
+ *   k_cache, v_cache : [n_pages, page, Hkv, d], both bf16 or both FP8 E4M3, of the same shape and strides; last axis
+ *       contiguous, rows 16-byte aligned, page % 16 == 0, d in {64, 128}, at most 2^26 elements from slot to slot.  Any
+ *       order of the outer axes in memory.  An FP8 element stands for its value times k_scale or v_scale (finite and
+ *       above 0; 1 for bf16).
+ *   pages    : [B, max_pages] i32: key j of sequence b is in slot j % page of page pages[b, j / page].  Entries past a
+ *       sequence's last key are not looked at.
+ *   kv_len   : [B] i32: keys of the sequence, its new tokens among them: token i of n has key and position
+ *       kv_len[b] - n + i.  Where that is negative the token has neither (a captured batch's unused places: kv_len 0).
+ *   seq_start: [B + 1] i32.
+ * The three arrays are read on the device only, so a captured graph serves every batch that fits.  Whatever they say,
+ * no access leaves the tensors.  A page number outside the cache, or more keys than max_pages has room for, is
+ * answered by NaN (see the entry points).  T * Hq < 2^31.
+ */
+
+/*
+ * The new tokens' way into the cache: per-head RMSNorm and rotation of queries and keys, the rotated queries to q_out,
+ * keys and values to their slots.
+ *   q : [T, Hq, d] bf16     k, v : [T, Hkv, d] bf16 (three parts of one projection's output, say)
+ *   q_norm, k_norm : [d] bf16, or null for no norm:  x' = x g / sqrt(mean x^2 + eps)
+ *   cos, sin : [positions, rot / 2] f32, or both null for no rotation; rot % 16 == 0, rot <= d.  The first rot values of
+ *       a head are rotated by their position's row: pairs (j, j + rot / 2), or (2 j, 2 j + 1) if interleaved != 0;
+ *       (a, b) becomes (a cos - b sin, b cos + a sin).
+ *   q_out : [T, Hq, d] bf16; may be q itself, any other overlap is undefined.
+ * All arithmetic is fp32 with one rounding at the end, to nearest even; FP8 codes saturate at 448.
+ * A token without a position gets 0 in q_out and no slot.  One whose page is not in the cache, or not in the table, is
+ * not cached.  One whose position the tables do not reach has NaN in the rotated values of its queries and its key.
+ * Two tokens of a call must not share a slot.
+ */
+RF_API rf_status rf_paged_append(const rf_tensor* q, const rf_tensor* k, const rf_tensor* v,
+                                 const rf_tensor* q_norm, const rf_tensor* k_norm, float eps,
+                                 const rf_tensor* cos, const rf_tensor* sin, int interleaved,
+                                 const rf_tensor* seq_start, const rf_tensor* kv_len, const rf_tensor* pages,
+                                 rf_tensor* k_cache, rf_tensor* v_cache, float k_scale, float v_scale,
+                                 rf_tensor* q_out, rf_stream stream);
+
+/*
+ * Attention of the new tokens over their sequences' caches (the cascade of rf_cascade_attention, GQA as there):
+ * a single token each, a few drafted ones, or a prompt's chunk, in any mixture.
+ *   q, o : [T, Hq, d] bf16, Hq % Hkv == 0.
+ *   causal != 0: token i of n sees keys j <= kv_len - n + i, otherwise all keys.  A row that sees none produces zeros,
+ *       and what an unseen slot holds (NaN too) does not show.
+ *   max_q : tokens of the longest sequence, for the choice of kernels; results are right for any value >= 0.
+ * Rows that see a key whose page is not in the cache are NaN (others of the same sequence may be), and so are all rows
+ * of a sequence with more keys than the table has room for.
+ */
+RF_API rf_status rf_paged_attention(const rf_tensor* q, const rf_tensor* k_cache, const rf_tensor* v_cache,
+                                    const rf_tensor* seq_start, const rf_tensor* kv_len, const rf_tensor* pages,
+                                    int64_t max_q, float scale, int causal, float k_scale, float v_scale,
+                                    rf_tensor* o, rf_stream stream);
+
+/*
+ * rf_paged_attention with device memory for partial states: the keys of long sequences are cut into chunks (their
+ * size is chosen on the device, from the lengths of the whole batch) whose states a second launch merges.
+ *   workspace : device memory, 16-byte aligned, at least
+ *       rf_paged_attention_workspace_bytes(q, k_cache, pages, max_q) bytes (which looks at shapes and types only);
+ *       contents need no initialisation and are undefined afterwards.  Too small or misaligned: RF_ERR_WORKSPACE.
+ *       Concurrent calls must not share a workspace.
+ * The size is 0 where no sequence can be long enough to be cut (the call is then rf_paged_attention) and for shapes
+ * that are refused, and at most 256 MiB.
+ */
+RF_API size_t rf_paged_attention_workspace_bytes(const rf_tensor* q, const rf_tensor* k_cache, const rf_tensor* pages,
+                                    int64_t max_q);
+RF_API rf_status rf_paged_attention_ws(const rf_tensor* q, const rf_tensor* k_cache, const rf_tensor* v_cache,
+                                    const rf_tensor* seq_start, const rf_tensor* kv_len, const rf_tensor* pages,
+                                    int64_t max_q, float scale, int causal, float k_scale, float v_scale,
+                                    rf_tensor* o, void* workspace, size_t workspace_bytes, rf_stream stream);
+
+/*
+ * Verification of drafted tokens against the target's probabilities, with given random numbers.  A sequence's rows
+ * r = 0 .. n (packed by seq_start as above) hold the target's probabilities p_r, the draft's q_r, and x_r, the token
+ * drafted from q_r; its last row has no draft:
+ *   a = the first r < n with u_accept[r] q_r(x_r) >= p_r(x_r), n if there is none;  x_0 .. x_{a-1} are accepted
+ *   w(t) = max(0, p_a(t) - q_a(t));  where a = n, or w is 0 all over: w = max(0, p_a)
+ *   the next token is the first t with w(0) + .. + w(t) > u_sample[b] sum_t w(t)
+ * so that every token is distributed as the target's own would be.  Comparisons and sums are in 64 bits.
+ *   target : [R, V] f32 or bf16, rows need not be normalised.  draft : the same shape and type, or null for drafts
+ *       without probabilities of their own (q = 1 at x_r).  Any row pitch and alignment.  V >= 1.
+ *   tokens : [R] i32 (x_r; entries of last rows are not looked at; a token outside 0 .. V-1 is refused)
+ *   u_accept : [R] f32, u_sample : [B] f32, uniform in [0, 1).   seq_start : [B + 1] i32
+ *   out : [R] i32: the accepted tokens, the next one, then -1.   accepted : [B] i32: a (0 for a sequence without rows)
+ * Weights that hold NaN or an infinity, or nothing above 0, give -1 for the next token.  Outputs must not overlap inputs.
+ */
+RF_API rf_status rf_verify_drafts(const rf_tensor* target, const rf_tensor* draft, const rf_tensor* tokens,
+                                  const rf_tensor* u_accept, const rf_tensor* u_sample, const rf_tensor* seq_start,
+                                  rf_tensor* out, rf_tensor* accepted, rf_stream stream);
+/*
+ * rf_verify_drafts with device memory for the sums over parts of a row, formed by a launch of their own: the same
+ * results.  Size and rules of the workspace as above (B sequences, V tokens); 0 for vocabularies of one part.
+ */
+RF_API size_t rf_verify_drafts_workspace_bytes(int64_t B, int64_t V);
+RF_API rf_status rf_verify_drafts_ws(const rf_tensor* target, const rf_tensor* draft, const rf_tensor* tokens,
+                                  const rf_tensor* u_accept, const rf_tensor* u_sample, const rf_tensor* seq_start,
+                                  rf_tensor* out, rf_tensor* accepted, void* workspace, size_t workspace_bytes,
+                                  rf_stream stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -42,6 +42,13 @@ ENTRY_POINTS = (
     "rf_fp8_quant_gemm",
     "rf_fp8_quant_gemm_workspace_bytes",
     "rf_fp8_quant_gemm_ws",
+    "rf_paged_append",
+    "rf_paged_attention",
+    "rf_paged_attention_workspace_bytes",
+    "rf_paged_attention_ws",
+    "rf_verify_drafts",
+    "rf_verify_drafts_workspace_bytes",
+    "rf_verify_drafts_ws",
 )
 # measurement aids and the fusion-level study, declared in include/rf_diag.h
 DIAG_ENTRY_POINTS = (
@@ -133,6 +140,21 @@ def load_library():
     lib.rf_fp8_quant_gemm_workspace_bytes.argtypes = [ctypes.c_int64, ctypes.c_int64, ctypes.c_int64]
     lib.rf_fp8_quant_gemm_ws.restype = ctypes.c_int
     lib.rf_fp8_quant_gemm_ws.argtypes = [P, P, P, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
+    F, I, I64, V, Z = ctypes.c_float, ctypes.c_int, ctypes.c_int64, ctypes.c_void_p, ctypes.c_size_t
+    lib.rf_paged_append.restype = I
+    lib.rf_paged_append.argtypes = [P, P, P, P, P, F, P, P, I, P, P, P, P, P, F, F, P, V]
+    lib.rf_paged_attention.restype = I
+    lib.rf_paged_attention.argtypes = [P, P, P, P, P, P, I64, F, I, F, F, P, V]
+    lib.rf_paged_attention_workspace_bytes.restype = Z
+    lib.rf_paged_attention_workspace_bytes.argtypes = [P, P, P, I64]
+    lib.rf_paged_attention_ws.restype = I
+    lib.rf_paged_attention_ws.argtypes = [P, P, P, P, P, P, I64, F, I, F, F, P, V, Z, V]
+    lib.rf_verify_drafts.restype = I
+    lib.rf_verify_drafts.argtypes = [P, P, P, P, P, P, P, P, V]
+    lib.rf_verify_drafts_workspace_bytes.restype = Z
+    lib.rf_verify_drafts_workspace_bytes.argtypes = [I64, I64]
+    lib.rf_verify_drafts_ws.restype = I
+    lib.rf_verify_drafts_ws.argtypes = [P, P, P, P, P, P, P, P, V, Z, V]
     lib.rf_diag_softmax_level.restype = ctypes.c_int
     lib.rf_diag_attention_wide.argtypes = [P, P, P, P, ctypes.c_float, ctypes.c_void_p]
     lib.rf_diag_attention_wide.restype = ctypes.c_int
@@ -333,6 +355,46 @@ def rf_fp8_quant_gemm(a, w, c=None, stream=None):
         c = torch.empty((a.shape[0], w.shape[0]), dtype=torch.bfloat16, device=a.device)
     _check((_call or _native()).fp8_quant_gemm(a, w, c, stream), "rf_fp8_quant_gemm")
     return c
+
+
+def rf_paged_append(q, k, v, k_cache, v_cache, seq_start, kv_len, pages, q_norm=None, k_norm=None, eps=1e-6, cos=None,
+                    sin=None, interleaved=False, k_scale=1.0, v_scale=1.0, q_out=None, stream=None):
+    """Norm and rotation of the packed new tokens' queries and keys, keys and values into their pages; returns the
+    queries (``q_out``, allocated if not given; may be ``q``).  ``q`` [T,Hq,d], ``k``, ``v`` [T,Hkv,d] bf16; caches
+    [n_pages,page,Hkv,d] bf16 or torch.float8_e4m3fn; ``seq_start`` [B+1], ``kv_len`` [B], ``pages`` [B,max_pages] int32;
+    ``cos``, ``sin`` [positions,rot/2] float32.  All tensors on the current device."""
+    if q_out is None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    _check((_call or _native()).paged_append(q, k, v, q_norm, k_norm, eps, cos, sin, interleaved, seq_start, kv_len, pages,
+                                             k_cache, v_cache, k_scale, v_scale, q_out, stream), "rf_paged_append")
+    return q_out
+
+
+def rf_paged_attention(q, k_cache, v_cache, seq_start, kv_len, pages, max_q, scale, causal=True, k_scale=1.0, v_scale=1.0,
+                       o=None, stream=None):
+    """Attention of the packed new tokens [T,Hq,d] over their sequences' pages; returns o (allocated if not given, rows
+    behind the last sequence then hold anything).  ``max_q``: tokens of the longest sequence (``q.shape[0]`` if unknown).
+    The workspace of rf_paged_attention_ws comes from torch's caching allocator, on the call's stream, and goes back to it
+    at return.  All tensors on the current device."""
+    if o is None:
+        o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    _check((_call or _native()).paged_attention(q, k_cache, v_cache, seq_start, kv_len, pages, max_q, scale, causal, k_scale,
+                                                v_scale, o, stream), "rf_paged_attention")
+    return o
+
+
+def rf_verify_drafts(target, draft, tokens, u_accept, u_sample, seq_start, out=None, accepted=None, stream=None):
+    """Accepts drafted tokens or replaces the first refused one; returns (out [R] int32: accepted tokens, the next one,
+    then -1; accepted [B] int32).  ``target``, ``draft`` [R,V] f32 or bf16 probabilities (``draft`` None: drafts without
+    any), ``tokens`` [R] int32, ``u_accept`` [R] and ``u_sample`` [B] float32 in [0,1), ``seq_start`` [B+1] int32.
+    Workspace as for rf_paged_attention.  All tensors on the current device."""
+    if out is None:
+        out = torch.empty(target.shape[0], dtype=torch.int32, device=target.device)
+    if accepted is None:
+        accepted = torch.empty(u_sample.shape[0], dtype=torch.int32, device=target.device)
+    _check((_call or _native()).verify_drafts(target, draft, tokens, u_accept, u_sample, seq_start, out, accepted, stream),
+           "rf_verify_drafts")
+    return out, accepted
 
 
 def rf_diag_softmax_level(x, y, level, ml_buf=None, stream=None):

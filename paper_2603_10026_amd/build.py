@@ -35,6 +35,11 @@ SOURCES = [
     "rmsnorm_gemm_rows.hip",
     "rmsnorm_gemm_two_pass.hip",
     "diag.hip",
+    # the operators of a serving step
+    "../csrc_serving/api_serving.hip",
+    "../csrc_serving/paged_append.hip",
+    "../csrc_serving/paged_attention_rows.hip",
+    "../csrc_serving/verify_drafts.hip",
 ]
 
 HIPCC_FLAGS = [
@@ -68,7 +73,7 @@ def build_library(verbose=True, jobs=8):
     procs = []
     objs = []
     for src in SOURCES:
-        obj = os.path.join(objdir, src.replace(".hip", ".o"))
+        obj = os.path.join(objdir, os.path.basename(src).replace(".hip", ".o"))
         objs.append(obj)
         cmd = [cc, *HIPCC_FLAGS, "-c", os.path.join(CSRC, src), "-o", obj]
         if verbose:

@@ -5,81 +5,16 @@
 
 #include <string.h>
 
+#include "rf_check.h"
 #include "rf_launch.h"
 
 static_assert(RF_MOE_ROUTING_NOALLOC_MAX_BYTES == rf::kMoeStaticScratchBytes, "header and kernels agree on the scratch size");
 
 namespace {
 
-inline size_t esize(rf_dtype t) { return t == RF_BF16 ? 2 : t == RF_FP8_E4M3 ? 1 : 4; }  // f32, i32: 4
-// `also`: one more dtype this argument may have (-1: none)
-inline bool dtype_ok(rf_dtype t, int also) {
-  return t == RF_F32 || t == RF_BF16 || (also >= 0 && (int)t == also);
-}
-
-// Structural checks common to every tensor argument.
-// (integer and FP8 tensors are accepted only where an entry point asks for them)
-rf_status check_tensor(const rf_tensor* t, int ndim_min, int ndim_max, int also = -1) {
-  if (t == nullptr) return RF_ERR_INVALID_ARG;
-  if (t->ndim < ndim_min || t->ndim > ndim_max) return RF_ERR_INVALID_ARG;
-  if (!dtype_ok(t->dtype, also)) return RF_ERR_UNSUPPORTED;
-  for (int i = 0; i < t->ndim; ++i) {
-    if (t->shape[i] < 0 || t->stride[i] < 0) return RF_ERR_INVALID_ARG;
-  }
-  return RF_OK;
-}
-
-int64_t numel(const rf_tensor* t) {
-  int64_t n = 1;
-  for (int i = 0; i < t->ndim; ++i) n *= t->shape[i];
-  return n;
-}
-
-bool same_shape(const rf_tensor* a, const rf_tensor* b) {
-  if (a->ndim != b->ndim) return false;
-  for (int i = 0; i < a->ndim; ++i)
-    if (a->shape[i] != b->shape[i]) return false;
-  return true;
-}
-
-bool is_contiguous(const rf_tensor* t) {
-  int64_t expect = 1;
-  for (int i = t->ndim - 1; i >= 0; --i) {
-    if (t->shape[i] != 1 && t->stride[i] != expect) return false;
-    expect *= t->shape[i];
-  }
-  return true;
-}
-
-// 16-byte alignment of the base pointer and of every outer stride.
-bool aligned16(const rf_tensor* t) {
-  if (reinterpret_cast<uintptr_t>(t->data) % 16 != 0) return false;
-  for (int i = 0; i + 1 < t->ndim; ++i)
-    if (t->shape[i] > 1 && (t->stride[i] * (int64_t)esize(t->dtype)) % 16 != 0) return false;
-  return true;
-}
-
-// Leading dims collapse to `rows` rows with a single pitch?
-bool collapse_rows(const rf_tensor* t, int64_t* rows, int64_t* pitch) {
-  const int nd = t->ndim;
-  int64_t r = 1;
-  for (int i = 0; i + 1 < nd; ++i) r *= t->shape[i];
-  *rows = r;
-  if (nd == 1) { *pitch = t->shape[0]; return true; }
-  *pitch = t->stride[nd - 2];
-  for (int i = nd - 3; i >= 0; --i) {
-    if (t->shape[i] == 1) continue;
-    if (t->stride[i] != t->stride[i + 1] * t->shape[i + 1]) return false;
-  }
-  if (r > 1 && *pitch < t->shape[nd - 1]) return false;
-  return true;
-}
+using namespace rf::check;
 
 rf::Strides4 strides4(const rf_tensor* t) { return {t->stride[0], t->stride[1], t->stride[2]}; }
-
-struct AttnArgs {
-  rf::AttnShape a;
-};
 
 // Shared validation of (q, k, v) for the attention entry points.
 rf_status check_qkv(const rf_tensor* q, const rf_tensor* k, const rf_tensor* v, rf::AttnShape* a) {
@@ -130,17 +65,24 @@ int rf_describe_cascade(const char* entry, rf_stage* out, int cap) {
   // max, sum of exponentials, TopK (a max-type reduction, Table 1)
   static const rf_stage kRouting[] = {
       {RF_RED_MAX, RF_COMB_ADD}, {RF_RED_SUM, RF_COMB_MUL}, {RF_RED_MAX, RF_COMB_ADD}};
+  // sum of squares (of a head, for its norm)
+  static const rf_stage kNorm[] = {{RF_RED_SUM, RF_COMB_MUL}};
+  // the first refused draft, the sum of what is left of the target, the first token past the draw (min-type reductions)
+  static const rf_stage kVerify[] = {{RF_RED_MIN, RF_COMB_ADD}, {RF_RED_SUM, RF_COMB_MUL}, {RF_RED_MIN, RF_COMB_ADD}};
   // abs-max, then the scaled sum
   static const rf_stage kQuant[] = {{RF_RED_MAX, RF_COMB_ADD}, {RF_RED_SUM, RF_COMB_MUL}};
   const rf_stage* src = nullptr;
   int n = 0;
   if (!strcmp(entry, "rf_safe_softmax")) { src = kSoftmax; n = 2; }
   else if (!strcmp(entry, "rf_cascade_attention") || !strcmp(entry, "rf_cascade_attention_ws") || !strcmp(entry, "rf_cascade_attention_splitk") ||
-           !strcmp(entry, "rf_merge_states")) { src = kAttention; n = 3; }
+           !strcmp(entry, "rf_merge_states") || !strcmp(entry, "rf_paged_attention") ||
+           !strcmp(entry, "rf_paged_attention_ws")) { src = kAttention; n = 3; }
   else if (!strcmp(entry, "rf_rmsnorm_gemm") || !strcmp(entry, "rf_rmsnorm_gemm_ws")) { src = kRms; n = 2; }
   else if (!strcmp(entry, "rf_variance")) { src = kRms; n = 2; }  // sum, then sum
   else if (!strcmp(entry, "rf_moe_routing")) { src = kRouting; n = 3; }
   else if (!strcmp(entry, "rf_fp8_quant_gemm") || !strcmp(entry, "rf_fp8_quant_gemm_ws")) { src = kQuant; n = 2; }
+  else if (!strcmp(entry, "rf_paged_append")) { src = kNorm; n = 1; }
+  else if (!strcmp(entry, "rf_verify_drafts") || !strcmp(entry, "rf_verify_drafts_ws")) { src = kVerify; n = 3; }
   else return -1;
   if (out != nullptr)
     for (int i = 0; i < n && i < cap; ++i) out[i] = src[i];

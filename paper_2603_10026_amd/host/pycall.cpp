@@ -327,6 +327,100 @@ PyObject* py_moe_routing_noalloc(PyObject*, PyObject* const* args, Py_ssize_t n)
   END_HANDLE_TH_ERRORS
 }
 
+// The serving operators take up to a dozen tensors, some of them optional (None: null).  They follow arrays on the
+// device, so a tensor that is not on the current device is refused here: the ABI cannot tell.
+template <int N>
+bool describe_here(PyObject* const* args, Py_ssize_t n, rf_tensor (&d)[N], rf_tensor* (&at)[N], const int (&from)[N],
+                   rf_stream* s, int* device, bool* here) {
+  *here = true;
+  int dev = -1;
+  for (int i = 0; i < N; ++i) {
+    PyObject* obj = args[from[i]];
+    at[i] = obj == Py_None ? nullptr : &d[i];
+    if (obj == Py_None) continue;
+    if (!describe(obj, &d[i], &dev)) return false;
+    if (THPVariable_Check(obj)) {
+      const at::Tensor& t = THPVariable_Unpack(obj);
+      *here = *here && t.is_cuda() && t.device().index() == c10::hip::current_device();
+    }
+  }
+  *device = dev;
+  return stream_of(args[n - 1], dev, s);
+}
+
+bool to_int64(PyObject* obj, int64_t* out) {  // int(obj)
+  PyObject* v = PyNumber_Long(obj);
+  if (v == nullptr) return false;
+  *out = PyLong_AsLongLong(v);
+  Py_DECREF(v);
+  return PyErr_Occurred() == nullptr;
+}
+
+// paged_append(q, k, v, q_norm, k_norm, eps, cos, sin, interleaved, seq_start, kv_len, pages, k_cache, v_cache, k_scale,
+//              v_scale, q_out, stream)
+PyObject* py_paged_append(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  rf_tensor d[13], *t[13];
+  float eps, ks, vs;
+  rf_stream s;
+  int device;
+  bool here;
+  if (!count(n, 18) || !describe_here<13>(args, n, d, t, {0, 1, 2, 3, 4, 6, 7, 9, 10, 11, 12, 13, 16}, &s, &device, &here) ||
+      !to_float(args[5], &eps) || !to_float(args[14], &ks) || !to_float(args[15], &vs))
+    return nullptr;
+  const int interleaved = PyObject_IsTrue(args[8]);
+  if (interleaved < 0) return nullptr;
+  if (!here) return PyLong_FromLong(RF_ERR_INVALID_ARG);
+  return call([&] {
+    return rf_paged_append(t[0], t[1], t[2], t[3], t[4], eps, t[5], t[6], interleaved, t[7], t[8], t[9], t[10], t[11], ks, vs,
+                           t[12], s);
+  });
+  END_HANDLE_TH_ERRORS
+}
+
+// paged_attention(q, k_cache, v_cache, seq_start, kv_len, pages, max_q, scale, causal, k_scale, v_scale, o, stream)
+PyObject* py_paged_attention(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  rf_tensor d[7], *t[7];
+  float scale, ks, vs;
+  int64_t max_q;
+  rf_stream s;
+  int device;
+  bool here;
+  if (!count(n, 13) || !describe_here<7>(args, n, d, t, {0, 1, 2, 3, 4, 5, 11}, &s, &device, &here) ||
+      !to_int64(args[6], &max_q) || !to_float(args[7], &scale) || !to_float(args[9], &ks) || !to_float(args[10], &vs))
+    return nullptr;
+  const int causal = PyObject_IsTrue(args[8]);
+  if (causal < 0) return nullptr;
+  if (!here) return PyLong_FromLong(RF_ERR_INVALID_ARG);
+  const size_t bytes = rf_paged_attention_workspace_bytes(t[0], t[1], t[5], max_q);
+  const Scratch scratch(bytes, device, s);
+  if (scratch.data() != nullptr)
+    return call([&] {
+      return rf_paged_attention_ws(t[0], t[1], t[2], t[3], t[4], t[5], max_q, scale, causal, ks, vs, t[6], scratch.data(), bytes, s);
+    });
+  return call([&] { return rf_paged_attention(t[0], t[1], t[2], t[3], t[4], t[5], max_q, scale, causal, ks, vs, t[6], s); });
+  END_HANDLE_TH_ERRORS
+}
+
+// verify_drafts(target, draft, tokens, u_accept, u_sample, seq_start, out, accepted, stream)
+PyObject* py_verify_drafts(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  rf_tensor d[8], *t[8];
+  rf_stream s;
+  int device;
+  bool here;
+  if (!count(n, 9) || !describe_here<8>(args, n, d, t, {0, 1, 2, 3, 4, 5, 6, 7}, &s, &device, &here)) return nullptr;
+  if (!here) return PyLong_FromLong(RF_ERR_INVALID_ARG);
+  const size_t bytes = t[0] != nullptr && t[4] != nullptr && t[0]->ndim == 2 && t[4]->ndim == 1
+                           ? rf_verify_drafts_workspace_bytes(t[4]->shape[0], t[0]->shape[1]) : 0;
+  const Scratch scratch(bytes, device, s);
+  if (scratch.data() != nullptr)
+    return call([&] { return rf_verify_drafts_ws(t[0], t[1], t[2], t[3], t[4], t[5], t[6], t[7], scratch.data(), bytes, s); });
+  return call([&] { return rf_verify_drafts(t[0], t[1], t[2], t[3], t[4], t[5], t[6], t[7], s); });
+  END_HANDLE_TH_ERRORS
+}
+
 // describe(tensor) -> the bytes of its rf_tensor
 PyObject* py_describe(PyObject*, PyObject* const* args, Py_ssize_t n) {
   HANDLE_TH_ERRORS
@@ -342,7 +436,7 @@ PyObject* py_describe(PyObject*, PyObject* const* args, Py_ssize_t n) {
 PyMethodDef methods[] = {
     RF_PY(init), RF_PY(describe), RF_PY(safe_softmax), RF_PY(cascade_attention), RF_PY(cascade_attention_splitk),
     RF_PY(merge_states), RF_PY(rmsnorm_gemm), RF_PY(variance), RF_PY(fp8_quant_gemm), RF_PY(moe_routing),
-    RF_PY(moe_routing_noalloc), {nullptr, nullptr, 0, nullptr}};
+    RF_PY(moe_routing_noalloc), RF_PY(paged_append), RF_PY(paged_attention), RF_PY(verify_drafts), {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_rfcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
