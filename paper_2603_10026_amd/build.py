@@ -38,7 +38,9 @@ SOURCES = [
     # the operators of a serving step
     "../csrc_serving/api_serving.hip",
     "../csrc_serving/paged_append.hip",
+    "../csrc_serving/paged_attention.hip",
     "../csrc_serving/paged_attention_rows.hip",
+    "../csrc_serving/paged_attention_tiles.hip",
     "../csrc_serving/verify_drafts.hip",
 ]
 

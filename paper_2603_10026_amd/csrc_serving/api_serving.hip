@@ -105,6 +105,7 @@ rf_status check_paged_attention(const rf_tensor* q, const rf_tensor* k_cache, co
   if ((st = check_paged(q, k_cache, v_cache, seq_start, kv_len, pages, k_scale, v_scale, &a->p)) != RF_OK) return st;
   if ((st = check_tokens(o, a->p.T, a->p.Hq, a->p.d)) != RF_OK) return st;
   if (max_q < 0) return RF_ERR_INVALID_ARG;
+  if (!rf::paged_attention_fits(a->p, max_q)) return RF_ERR_UNSUPPORTED;
   a->q = q->data;
   a->k_cache = k_cache->data;
   a->v_cache = v_cache->data;
@@ -242,7 +243,7 @@ rf_status rf_paged_attention(const rf_tensor* q, const rf_tensor* k_cache, const
 size_t rf_paged_attention_workspace_bytes(const rf_tensor* q, const rf_tensor* k_cache, const rf_tensor* pages,
                                           int64_t max_q) {
   rf::Paged p{};
-  if (paged_shape(q, k_cache, pages, &p) != RF_OK || empty(p) || max_q < 0) return 0;
+  if (paged_shape(q, k_cache, pages, &p) != RF_OK || empty(p) || max_q < 0 || !rf::paged_attention_fits(p, max_q)) return 0;
   return rf::paged_attention_bytes(p, max_q);
 }
 

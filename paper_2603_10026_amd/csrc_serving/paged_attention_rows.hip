@@ -21,7 +21,7 @@
 // sums the rounded ones, so that the part of the error that all keys share cancels.  Everything else is fp32.
 #include <math.h>
 
-#include "serving_device.h"
+#include "paged_attention.h"
 
 namespace rf {
 
@@ -29,20 +29,8 @@ namespace {
 
 constexpr int kWaves = 4, kStepKeys = 32, kChunkStep = kWaves * kStepKeys;
 
-struct RowsArgs {
-  Paged p;
-  Deal deal;
-  const bf16_t* q;
-  const unsigned char *k, *v;
-  bf16_t* o;
-  Strides2 sq, so;
-  float scale_log2e, v_scale;
-  int causal;
-  float *part_acc, *part_m, *part_l;
-};
-
 template <int D, int NR, bool FP8>
-__global__ __launch_bounds__(kWaves* kWave, 2) void paged_rows_kernel(const RowsArgs a) {
+__global__ __launch_bounds__(kWaves* kWave, 2) void paged_rows_kernel(const PagedArgs a) {
   constexpr int ES = FP8 ? 1 : 2;            // bytes of a cached element
   constexpr int KS = D / 32;                 // contraction steps of S^T
   constexpr int DPL = D / 16;                // values of a V row a lane holds
@@ -68,7 +56,9 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void paged_rows_kernel(const Rows
   const int unit = __builtin_amdgcn_readfirstlane(blockIdx.x / p.Hkv);
   const int hk = __builtin_amdgcn_readfirstlane(blockIdx.x - unit * p.Hkv);
   Share w;
-  if (!find_share(p, a.deal, unit, false, &w)) return;
+  const bool found = find_share(p, a.deal, unit, &w);
+  if (hk == 0 && wave == 0) note_tile(a, unit, found, w);
+  if (!found) return;
 
   const int rows = w.s.n * p.group;
   const int r0 = w.tile * R;
@@ -377,150 +367,20 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void paged_rows_kernel(const Rows
   }
 }
 
-// O of the tiles in several chunks, from their states: a workgroup takes 4 rows of a tile, one after the other, 32 (16)
-// lanes a row of 128 (64) values and the chunks dealt to the groups of lanes.
-constexpr int kJoinRows = 4, kJoinThreads = 256;
-
-template <int D>
-__global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(const RowsArgs a) {
-  constexpr int kQuads = D / 4, kGroups = kJoinThreads / kQuads, U = 4;
-  __shared__ __attribute__((aligned(16))) float s_acc[kGroups][D];
-  __shared__ float s_m[kGroups], s_l[kGroups];
-  const Paged& p = a.p;
-  const int R = 1 << a.deal.rows_log2, parts = R / kJoinRows;
-  const int part = __builtin_amdgcn_readfirstlane(blockIdx.x % parts);
-  const int unit = __builtin_amdgcn_readfirstlane(blockIdx.x / parts / p.Hkv);
-  const int hk = __builtin_amdgcn_readfirstlane(blockIdx.x / parts % p.Hkv);
-  Share w;
-  if (!find_share(p, a.deal, unit, true, &w) || w.chunks == 1) return;
-  const int rows = w.s.n * p.group, grp = threadIdx.x / kQuads, c4 = threadIdx.x % kQuads;
-  const int64_t pitch = (int64_t)p.Hkv * R;  // rows of the workspace from one chunk to the next
-  for (int rr = 0; rr < kJoinRows; ++rr) {
-    const int in_tile = part * kJoinRows + rr, r = w.tile * R + in_tile;
-    if (r >= rows) return;
-    const int64_t row = ((int64_t)w.slot * p.Hkv + hk) * R + in_tile;
-    float m = -INFINITY, l = 0.f;
-    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-    for (int c0 = grp; c0 < w.chunks; c0 += U * kGroups) {
-      float mc[U], lc[U];
-      f32x4 ac[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int64_t at = row + min(c0 + u * kGroups, w.chunks - 1) * pitch;
-        mc[u] = a.part_m[at];
-        lc[u] = a.part_l[at];
-        ac[u] = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(a.part_acc + at * D + 4 * c4));
-      }
-      float m_new = m;
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        mc[u] = c0 + u * kGroups < w.chunks ? mc[u] : -INFINITY;
-        m_new = fmaxf(m_new, mc[u]);
-      }
-      const float m_use = m_new == -INFINITY ? 0.f : m_new;
-      const float corr = fast_exp2(m - m_use);
-      l *= corr;
-      sum *= corr;
-      m = m_new;
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (mc[u] == -INFINITY) continue;  // an empty state
-        const float wgt = fast_exp2(mc[u] - m_use);
-        l += lc[u] * wgt;
-        sum += ac[u] * wgt;
-      }
-    }
-    __syncthreads();  // the row before has been read
-    *reinterpret_cast<f32x4*>(&s_acc[grp][4 * c4]) = sum;
-    if (c4 == 0) {
-      s_m[grp] = m;
-      s_l[grp] = l;
-    }
-    __syncthreads();
-    if (threadIdx.x < kQuads) {
-      m = -INFINITY;
-#pragma unroll
-      for (int i = 0; i < kGroups; ++i) m = fmaxf(m, s_m[i]);
-      const float m_use = m == -INFINITY ? 0.f : m;
-      l = 0.f;
-      sum = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int i = 0; i < kGroups; ++i) {
-        const float wgt = fast_exp2(s_m[i] - m_use);
-        l += s_l[i] * wgt;
-        sum += *reinterpret_cast<const f32x4*>(&s_acc[i][4 * c4]) * wgt;
-      }
-      const float inv = l == 0.f ? 0.f : a.v_scale / l;
-      const int i = r / p.group, h = hk * p.group + r - i * p.group;
-      u32x2 w2;
-      w2[0] = pack_bf16(sum[0] * inv, sum[1] * inv);
-      w2[1] = pack_bf16(sum[2] * inv, sum[3] * inv);
-      *reinterpret_cast<u32x2*>(a.o + (int64_t)(w.s.row0 + i) * a.so.t + (int64_t)h * a.so.h + 4 * c4) = w2;
-    }
-  }
-}
-
-// Tiles of 1 << rows_log2 rows that a launch may meet at most.
-int64_t most_tiles(const Paged& p, int rows_log2) {
-  return (((int64_t)p.T * p.group) >> rows_log2) + (p.B < p.T ? p.B : p.T);
-}
-
-constexpr int kLeastChunk = 256, kWorkgroups = 1024;
-
-int rows_log2_of(const Paged& p, int64_t max_q) {
-  const int64_t most = max_q < p.T ? max_q : p.T;
-  return most * p.group <= 16 ? 4 : 5;
-}
-
-int chunk_target(const Paged& p) {
-  // no sequence is long enough, or there are more than enough workgroups without cutting any
-  if ((int64_t)p.table_len * p.page <= kLeastChunk || p.Hkv > kWorkgroups) return 0;
-  return (kWorkgroups + p.Hkv - 1) / p.Hkv;
-}
-
 }  // namespace
 
-size_t paged_attention_bytes(const Paged& p, int64_t max_q) {
-  if (p.T == 0 || p.B == 0) return 0;
-  const int target = chunk_target(p);
-  return ((size_t)2 * target * p.Hkv << rows_log2_of(p, max_q)) * (p.d + 2) * sizeof(float);
-}
-
-hipError_t launch_paged_attention(const PagedAttention& x, void* workspace, hipStream_t s) {
-  const Paged& p = x.p;
-  RowsArgs a;
-  a.p = p;
-  a.q = (const bf16_t*)x.q;
-  a.k = (const unsigned char*)x.k_cache;
-  a.v = (const unsigned char*)x.v_cache;
-  a.o = (bf16_t*)x.o;
-  a.sq = x.sq;
-  a.so = x.so;
-  a.scale_log2e = x.scale_log2e;
-  a.v_scale = x.v_scale;
-  a.causal = x.causal;
-  const int lg = rows_log2_of(p, x.max_q);
-  a.deal = Deal{lg, 0, INT32_MAX, workspace != nullptr ? chunk_target(p) : 0, kLeastChunk};
-  const int64_t tiles = most_tiles(p, lg);
-  const int64_t slots = ((int64_t)2 * a.deal.target * p.Hkv) << lg;
-  a.part_acc = (float*)workspace;
-  a.part_m = a.part_acc + slots * p.d;
-  a.part_l = a.part_m + slots;
-  const int64_t grid = (tiles + a.deal.target) * p.Hkv, join = tiles * p.Hkv * ((1 << lg) / kJoinRows);
-  if (grid > UINT32_MAX / (kWaves * kWave) || join > UINT32_MAX / kJoinThreads) return hipErrorInvalidValue;
+hipError_t launch_paged_rows(const PagedArgs& a, bool fp8, hipStream_t s) {
+  const int64_t grid = ((int64_t)a.n_tiles + a.deal.target) * a.p.Hkv;
+  if (grid > UINT32_MAX / (kWaves * kWave)) return hipErrorInvalidValue;
 #define RF_ROWS(DD, NN, F8) \
   hipLaunchKernelGGL((paged_rows_kernel<DD, NN, F8>), dim3((unsigned)grid), dim3(kWaves * kWave), 0, s, a)
-#define RF_ROWS_D(DD)                                              \
-  if (lg == 4) { if (x.fp8) RF_ROWS(DD, 1, true); else RF_ROWS(DD, 1, false); } \
-  else { if (x.fp8) RF_ROWS(DD, 2, true); else RF_ROWS(DD, 2, false); }         \
-  if (a.deal.target > 0)                                           \
-    hipLaunchKernelGGL((paged_join_kernel<DD>), dim3((unsigned)join), dim3(kJoinThreads), 0, s, a)
-  if (p.d == 128) {
+#define RF_ROWS_D(DD)                                                                        \
+  if (a.deal.rows_log2 == 4) { if (fp8) RF_ROWS(DD, 1, true); else RF_ROWS(DD, 1, false); } \
+  else { if (fp8) RF_ROWS(DD, 2, true); else RF_ROWS(DD, 2, false); }
+  if (a.p.d == 128) {
     RF_ROWS_D(128);
-  } else if (p.d == 64) {
-    RF_ROWS_D(64);
   } else {
-    return hipErrorInvalidValue;
+    RF_ROWS_D(64);
   }
 #undef RF_ROWS_D
 #undef RF_ROWS

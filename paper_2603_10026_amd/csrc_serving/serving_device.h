@@ -71,14 +71,16 @@ struct Deal {
 struct Share {
   Sequence s;
   int b, tile, chunk, chunks, chunk_keys;
-  int slot;  // of this share among those of sequences in several chunks
+  int slot;        // of this share among those of sequences in several chunks
+  int tile_index;  // of its tile among all tiles
+  int all_shares, all_tiles;  // of the batch (where there is no such share)
 };
 
-// Share number `unit` (by_tile: the first chunk of tile number `unit`) of the batch; false past the last one.  Shares
+// Share number `unit` of the batch; false past the last one.  Shares
 // are counted sequence by sequence, tile by tile.  There are at most target + tiles of them, and at most 2 target with
 // more than one chunk to their tile: such a tile has over chunk_keys keys, so ceil(keys / chunk_keys) is below twice
 // keys / chunk_keys, and the sum of all keys / chunk_keys is at most target.
-__device__ __forceinline__ bool find_share(const Paged& p, const Deal& d, int unit, bool by_tile, Share* out) {
+__device__ __forceinline__ bool find_share(const Paged& p, const Deal& d, int unit, Share* out) {
   const int lane = threadIdx.x & 63;
   auto load = [&](int b0, int* tiles) {
     Sequence s{0, 0, 0, false};
@@ -104,22 +106,23 @@ __device__ __forceinline__ bool find_share(const Paged& p, const Deal& d, int un
     const float share = fminf(ceilf(wave_sum(keys) / (float)d.target * 1.0001f), 2e9f);
     chunk_keys = max(d.least, ((int)share + 127) & ~127);
   }
-  int base = 0, slot_base = 0;
+  int base = 0, slot_base = 0, tile_base = 0;
   for (int b0 = 0;;) {
-    const int chunks = s.len <= chunk_keys ? 1 : (s.len + chunk_keys - 1) / chunk_keys;
-    const int mine = by_tile ? tiles : tiles * chunks;
-    const int upto = wave_inclusive_scan(mine);
-    const int slots = chunks > 1 ? tiles * chunks : 0;
-    const int slots_upto = wave_inclusive_scan(slots);
+    const int chunks = s.len <= chunk_keys ? 1 : (int)(((unsigned)s.len + chunk_keys - 1) / (unsigned)chunk_keys);
+    const int upto = wave_inclusive_scan(tiles * chunks);
+    const int slots_upto = wave_inclusive_scan(chunks > 1 ? tiles * chunks : 0);
+    const int tiles_upto = wave_inclusive_scan(tiles);
     const uint64_t past = __builtin_amdgcn_ballot_w64(base + upto > unit);
     if (past != 0) {
       const int f = __ffsll((unsigned long long)past) - 1;
       auto get = [&](int v) { return __builtin_amdgcn_readlane(v, f); };
-      const int at = unit - (base + get(upto) - get(mine));
       out->chunks = get(chunks);
-      out->tile = by_tile ? at : __builtin_amdgcn_readfirstlane(at / out->chunks);
-      out->chunk = by_tile ? 0 : at - out->tile * out->chunks;
-      out->slot = slot_base + get(slots_upto) - get(slots) + out->tile * out->chunks + out->chunk;
+      const int units = get(tiles) * out->chunks;
+      const int at = unit - (base + get(upto) - units);
+      out->tile = out->chunks == 1 ? at : __builtin_amdgcn_readfirstlane(at / out->chunks);
+      out->chunk = at - out->tile * out->chunks;
+      out->slot = slot_base + get(slots_upto) - units + at;
+      out->tile_index = tile_base + get(tiles_upto) - get(tiles) + out->tile;
       out->b = b0 + f;
       out->chunk_keys = __builtin_amdgcn_readfirstlane(chunk_keys);
       out->s.row0 = get(s.row0);
@@ -130,8 +133,13 @@ __device__ __forceinline__ bool find_share(const Paged& p, const Deal& d, int un
     }
     base += __builtin_amdgcn_readlane(upto, 63);
     slot_base += __builtin_amdgcn_readlane(slots_upto, 63);
+    tile_base += __builtin_amdgcn_readlane(tiles_upto, 63);
     b0 += 64;
-    if (b0 >= p.B) return false;
+    if (b0 >= p.B) {
+      out->all_shares = base;
+      out->all_tiles = tile_base;
+      return false;
+    }
     s = load(b0, &tiles);
   }
 }
@@ -146,5 +154,12 @@ __device__ __forceinline__ uint32_t fp8_hi_to_bf16(uint32_t w) {
 
 // Nonzero where one of two packed bf16 values is an infinity or NaN (its exponent all ones).
 __device__ __forceinline__ uint32_t not_finite(uint32_t x) { return ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
+
+// Element `at` of a cache as bf16.
+template <bool FP8>
+__device__ __forceinline__ uint32_t cached_bf16(const unsigned char* cache, int64_t at) {
+  if constexpr (FP8) return fp8_lo_to_bf16(cache[at]) & 0xffffu;
+  return reinterpret_cast<const bf16_t*>(cache)[at];
+}
 
 }  // namespace rf

@@ -42,6 +42,7 @@ struct PagedAttention {
   int causal, fp8;
   int64_t max_q;               // tokens of the longest sequence, for the choice of kernels
 };
+bool paged_attention_fits(const Paged& p, int64_t max_q);  // whether its launches can be that large
 // Device memory that launch_paged_attention takes for the states of split sequences; 0 where no sequence is split.
 size_t paged_attention_bytes(const Paged& p, int64_t max_q);
 // workspace: that many bytes, 16-byte aligned, or null: no sequence is split then.
