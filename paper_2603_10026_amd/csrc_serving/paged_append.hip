@@ -7,7 +7,8 @@
 // in fp32, rounded once, to bf16 or to the cache's FP8 codes.  A token's position is len - n + i, its place in the cache.
 //
 // What bounds it is memory: 2 bytes a value in, 2 (1) out, one pass.  A head's values lie in 16 (8) lanes of 8, so the
-// sum of squares is a few lane exchanges and the partner of a rotated value is a fixed number of lanes away.  The
+// sum of squares is a few lane exchanges and the partner of a rotated value is a fixed number of lanes away (its exchange
+// through the vector unit instead of LDS: 1 us of 44).  The
 // tables' 8 bytes a pair would be twice the values' own traffic if every head read them: a wavefront holds a token's
 // angles in registers and goes over several of its heads.
 #include "serving_device.h"
@@ -35,21 +36,54 @@ __device__ __forceinline__ u32x2 fp8_of(const float* y, float scale) {
   return r;
 }
 
-// parts: how many wavefronts share a token's heads.
-template <int D, bool FP8>
-__global__ __launch_bounds__(kThreads) void paged_append_kernel(const PagedAppend a, int parts) {
+// parts: how many wavefronts share a token's heads; U: turns of a wavefront whose loads are under way at once;
+// past: results go past the caches.
+template <int D, bool FP8, int U>
+__global__ __launch_bounds__(kThreads) void paged_append_kernel(const PagedAppend a, int parts, bool past) {
   constexpr int kLanes = D / 8, kHeads = kWave / kLanes;  // lanes a head, heads a wavefront turns over at once
-  constexpr int U = 2;                                     // ... and how many of these are under way
   const Paged& p = a.p;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane((blockIdx.x * kThreads + threadIdx.x) >> 6);
-  const int t = __builtin_amdgcn_readfirstlane(wave / parts), part = wave - t * parts;
+  const int t = __builtin_amdgcn_readfirstlane((unsigned)wave / (unsigned)parts), part = wave - t * parts;
   if (t >= p.T) return;
-  const int b = __builtin_amdgcn_readfirstlane(find_start(p.seq_start, p.B + 1, t));
-  if (b < 0 || b >= p.B) return;  // before the first sequence, or behind the last
-  const Sequence s = load_sequence(p, b);
+
+  const int heads = p.Hq + 2 * p.Hkv, q_end = p.Hq, k_end = p.Hq + p.Hkv;
+  const int e0 = 8 * (lane % kLanes), sub = lane / kLanes;
+  const int turn = kHeads * parts;
+  u32x4 x[U];
+  auto load = [&](int h0) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int h = h0 + u * turn + sub;
+      const bf16_t* src = h < q_end   ? (const bf16_t*)a.q + (int64_t)t * a.sq.t + (int64_t)h * a.sq.h
+                          : h < k_end ? (const bf16_t*)a.k + (int64_t)t * a.sk.t + (int64_t)(h - q_end) * a.sk.h
+                                      : (const bf16_t*)a.v + (int64_t)t * a.sv.t + (int64_t)(h - k_end) * a.sv.h;
+      x[u] = u32x4{0u, 0u, 0u, 0u};
+      if (h < heads) x[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src + e0));
+    }
+  };
+  // The first values need nothing but the token's number: they are on their way while the arrays say where it belongs.
+  load(part * kHeads);
+
+  int b;
+  Sequence s;
+  int64_t len;
+  if (p.B < kWave) {
+    // every sequence to a lane: one trip for all that the arrays say
+    const int start = p.seq_start[min(lane, p.B)], keys = p.kv_len[min(lane, p.B - 1)];
+    b = __builtin_amdgcn_readfirstlane(__popcll(__builtin_amdgcn_ballot_w64(lane <= p.B && start <= t)) - 1);
+    if (b < 0 || b >= p.B) return;  // before the first sequence, or behind the last
+    s.row0 = min(max(__builtin_amdgcn_readlane(start, b), 0), p.T);
+    s.n = min(max(__builtin_amdgcn_readlane(start, b + 1), s.row0), p.T) - s.row0;
+    len = __builtin_amdgcn_readlane(keys, b);
+  } else {
+    b = __builtin_amdgcn_readfirstlane(find_start(p.seq_start, p.B + 1, t));
+    if (b < 0 || b >= p.B) return;
+    s = load_sequence(p, b);
+    len = p.kv_len[b];
+  }
   if (t < s.row0 || t >= s.row0 + s.n) return;
-  const int64_t pos = (int64_t)p.kv_len[b] - s.n + (t - s.row0);  // its key's place; negative: it has none
+  const int64_t pos = len - s.n + (t - s.row0);  // its key's place; negative: it has none
 
   int64_t slot = -1;
   if (pos >= 0 && pos < capacity_of(p)) {
@@ -58,7 +92,6 @@ __global__ __launch_bounds__(kThreads) void paged_append_kernel(const PagedAppen
     if (id >= 0 && id < p.n_pages) slot = (int64_t)id * p.page_stride + (int64_t)((int)pos - at * p.page) * p.slot_stride;
   }
 
-  const int e0 = 8 * (lane % kLanes), sub = lane / kLanes;
   // ---- angles: y = x c + partner s, with the sign of s ----
   const bool turns = e0 < a.rot;
   float c[8], sn[8];
@@ -101,20 +134,12 @@ __global__ __launch_bounds__(kThreads) void paged_append_kernel(const PagedAppen
   if (a.q_norm != nullptr) Elem<bf16_t>::unpack(*reinterpret_cast<const u32x4*>((const bf16_t*)a.q_norm + e0), gq);
   if (a.k_norm != nullptr) Elem<bf16_t>::unpack(*reinterpret_cast<const u32x4*>((const bf16_t*)a.k_norm + e0), gk);
 
-  const int heads = p.Hq + 2 * p.Hkv;
-  const int q_end = p.Hq, k_end = p.Hq + p.Hkv;
-  const int turn = kHeads * parts;
+  auto store = [&](auto* at, auto w) {
+    if (past) __builtin_nontemporal_store(w, at);
+    else *at = w;
+  };
   for (int h0 = part * kHeads; h0 < heads; h0 += U * turn) {
-    u32x4 x[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int h = h0 + u * turn + sub;
-      const bf16_t* src = h < q_end   ? (const bf16_t*)a.q + (int64_t)t * a.sq.t + (int64_t)h * a.sq.h
-                          : h < k_end ? (const bf16_t*)a.k + (int64_t)t * a.sk.t + (int64_t)(h - q_end) * a.sk.h
-                                      : (const bf16_t*)a.v + (int64_t)t * a.sv.t + (int64_t)(h - k_end) * a.sv.h;
-      x[u] = u32x4{0u, 0u, 0u, 0u};
-      if (h < heads) x[u] = *reinterpret_cast<const u32x4*>(src + e0);
-    }
+    if (h0 != part * kHeads) load(h0);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int h = h0 + u * turn + sub;
@@ -137,6 +162,10 @@ __global__ __launch_bounds__(kThreads) void paged_append_kernel(const PagedAppen
         if (a.interleaved) {
 #pragma unroll
           for (int i = 0; i < 8; ++i) y[i] = fmaf(f[i], c[i], f[i ^ 1] * sn[i]);
+        } else if (D == 128 && a.rot == 128) {
+          // (half a row of 16 lanes away: a lane exchange of the vector unit)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) y[i] = fmaf(f[i], c[i], dpp_f32<0x128>(f[i]) * sn[i]);
         } else {
 #pragma unroll
           for (int i = 0; i < 8; ++i) y[i] = fmaf(f[i], c[i], __shfl(f[i], partner, 64) * sn[i]);
@@ -151,12 +180,12 @@ __global__ __launch_bounds__(kThreads) void paged_append_kernel(const PagedAppen
       if (is_q) {
         // (a token without a place, which no key answers either, is 0)
         const u32x4 w = pos < 0 ? u32x4{0u, 0u, 0u, 0u} : Elem<bf16_t>::pack(y);
-        *reinterpret_cast<u32x4*>((bf16_t*)a.q_out + (int64_t)t * a.so.t + (int64_t)h * a.so.h + e0) = w;
+        store(reinterpret_cast<u32x4*>((bf16_t*)a.q_out + (int64_t)t * a.so.t + (int64_t)h * a.so.h + e0), w);
       } else if (slot >= 0) {
         const int64_t at = slot + (int64_t)(is_v ? h - k_end : h - q_end) * p.head_stride + e0;
         unsigned char* cache = (unsigned char*)(is_v ? a.v_cache : a.k_cache);
-        if constexpr (FP8) *reinterpret_cast<u32x2*>(cache + at) = fp8_of(y, is_v ? a.v_scale : a.k_scale);
-        else *reinterpret_cast<u32x4*>(cache + 2 * at) = is_v ? x[u] : Elem<bf16_t>::pack(y);
+        if constexpr (FP8) store(reinterpret_cast<u32x2*>(cache + at), fp8_of(y, is_v ? a.v_scale : a.k_scale));
+        else store(reinterpret_cast<u32x4*>(cache + 2 * at), is_v ? x[u] : Elem<bf16_t>::pack(y));
       }
     }
   }
@@ -164,18 +193,37 @@ __global__ __launch_bounds__(kThreads) void paged_append_kernel(const PagedAppen
 
 }  // namespace
 
+// A few tokens: a wavefront for every turn over a token's heads, since the time is the trips to memory one behind the
+// other.  Many: three turns under way at once, two rounds of them or one, which leaves a few wavefronts' work to every
+// SIMD.  us, U = 3 and 2 to 4 wavefronts a token / U = 1 and one for each turn / one wavefront with U = 2, d = 128,
+// 32 + 2 x 8 heads: 48 tokens 4.7 / 3.6 / 9.9, 256 tokens 5.3 / 4.8 / 10.6, 1000 tokens 8.1 / 11 / 14.4, 8500 tokens
+// 42.2 / 60 / 46.0.  From 8 MiB on results are written past the caches, which would not keep them: 25000 tokens
+// 110 us (5.7 TB/s) and 122 without, 1000 tokens 8.1 and 10.1, but 256 tokens 5.1 and 4.8.
 hipError_t launch_paged_append(const PagedAppend& a, hipStream_t s) {
-  const int parts = 1;
-  const int64_t grid = ((int64_t)a.p.T * parts + kThreads / kWave - 1) / (kThreads / kWave);
+  const int64_t T = a.p.T, heads = a.p.Hq + 2 * (int64_t)a.p.Hkv;
+  const int per_turn = kWave * 8 / a.p.d;
+  const int64_t turns = (heads + per_turn - 1) / per_turn;
+  const bool few = T <= 512;
+  const int64_t least = (turns + 5) / 6, most = (turns + 2) / 3, wanted = (16384 + T - 1) / T;
+  const int64_t parts = few ? turns : wanted < least ? least : wanted < most ? wanted : most;
+  const bool past = T * heads * a.p.d * 2 >= (8 << 20);
+  const int64_t grid = (T * parts + kThreads / kWave - 1) / (kThreads / kWave);
   if (grid > UINT32_MAX / kThreads) return hipErrorInvalidValue;
-#define RF_APPEND(DD, F8) \
-  hipLaunchKernelGGL((paged_append_kernel<DD, F8>), dim3((unsigned)grid), dim3(kThreads), 0, s, a, parts)
+#define RF_APPEND(DD, F8)                                                                                        \
+  if (few) hipLaunchKernelGGL((paged_append_kernel<DD, F8, 1>), dim3((unsigned)grid), dim3(kThreads), 0, s, a, (int)parts, past); \
+  else hipLaunchKernelGGL((paged_append_kernel<DD, F8, 3>), dim3((unsigned)grid), dim3(kThreads), 0, s, a, (int)parts, past)
   if (a.p.d == 128) {
-    if (a.fp8) RF_APPEND(128, true);
-    else RF_APPEND(128, false);
+    if (a.fp8) {
+      RF_APPEND(128, true);
+    } else {
+      RF_APPEND(128, false);
+    }
   } else if (a.p.d == 64) {
-    if (a.fp8) RF_APPEND(64, true);
-    else RF_APPEND(64, false);
+    if (a.fp8) {
+      RF_APPEND(64, true);
+    } else {
+      RF_APPEND(64, false);
+    }
   } else {
     return hipErrorInvalidValue;
   }

@@ -333,7 +333,7 @@ template <int N>
 bool describe_here(PyObject* const* args, Py_ssize_t n, rf_tensor (&d)[N], rf_tensor* (&at)[N], const int (&from)[N],
                    rf_stream* s, int* device, bool* here) {
   *here = true;
-  int dev = -1;
+  int dev = -1, first = -1;
   for (int i = 0; i < N; ++i) {
     PyObject* obj = args[from[i]];
     at[i] = obj == Py_None ? nullptr : &d[i];
@@ -341,9 +341,12 @@ bool describe_here(PyObject* const* args, Py_ssize_t n, rf_tensor (&d)[N], rf_te
     if (!describe(obj, &d[i], &dev)) return false;
     if (THPVariable_Check(obj)) {
       const at::Tensor& t = THPVariable_Unpack(obj);
-      *here = *here && t.is_cuda() && t.device().index() == c10::hip::current_device();
+      const int index = t.is_cuda() ? (int)t.device().index() : -2;
+      if (first == -1) first = index;
+      *here = *here && index >= 0 && index == first;
     }
   }
+  if (*here && first >= 0) *here = first == c10::hip::current_device();
   *device = dev;
   return stream_of(args[n - 1], dev, s);
 }
