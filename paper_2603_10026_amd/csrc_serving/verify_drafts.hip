@@ -10,19 +10,21 @@
 // fp32 sums that are off by 1e-7 would move one draw in a hundred).
 //
 // What bounds it is one row of p and of q for each sequence.  A row is cut into slices: the first launch finds a
-// (every workgroup for itself: two gathered values a draft) and sums its slice, the second finds the slice that the
-// draw falls into and then the token inside it.  Without a workspace one workgroup goes over all slices of a sequence.
+// (every workgroup for itself: two gathered values a draft, three dependent trips to memory) and sums its slice, the
+// second finds the slice that the draw falls into and then the token inside it.  Without a workspace one workgroup goes
+// over all slices of a sequence.
 #include "serving_device.h"
 
 namespace rf {
 
 namespace {
 
-constexpr int kThreads = 256, kWaves = kThreads / kWave;
-constexpr int kSlices = 64;       // at most, of a row
-constexpr int kLeastSlice = 4096; // values
+constexpr int kSumThreads = 256, kDrawThreads = 1024;
+constexpr int kSlices = 64;       // at most, of a row: a lane each
+constexpr int kMostWaves = kDrawThreads / kWave;
 
 // Sum over the workgroup's threads, in every one of them.
+template <int THREADS>
 __device__ __forceinline__ double group_sum(double v, double* s_red) {
 #pragma unroll
   for (int m = 1; m < 64; m <<= 1) v += __shfl_xor(v, m, 64);
@@ -31,7 +33,18 @@ __device__ __forceinline__ double group_sum(double v, double* s_red) {
   __syncthreads();
   v = 0;
 #pragma unroll
-  for (int i = 0; i < kWaves; ++i) v += s_red[i];
+  for (int i = 0; i < THREADS / kWave; ++i) v += s_red[i];
+  return v;
+}
+
+// Inclusive sum over the lanes up to this one.
+__device__ __forceinline__ double scan(double v) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const double o = __shfl_up(v, d, 64);
+    if (lane >= d) v += o;
+  }
   return v;
 }
 
@@ -67,25 +80,27 @@ struct Row {
       w[i] = d < 0 || t0 + i == token ? 0.0 : d;  // (NaN stays)
     }
   }
+  template <int THREADS>
   __device__ __forceinline__ double slice_sum(int64_t lo, int64_t hi, double* s_red) const {
     constexpr int N = Elem<T>::kPerVec;
     double sum = 0;
-    for (int64_t t = lo + threadIdx.x * N; t < hi; t += kThreads * N) {
+#pragma unroll 2
+    for (int64_t t = lo + threadIdx.x * N; t < hi; t += THREADS * N) {
       double w[N];
       weights(t, w);
 #pragma unroll
       for (int i = 0; i < N; ++i) sum += w[i];
     }
-    return group_sum(sum, s_red);
+    return group_sum<THREADS>(sum, s_red);
   }
-  // The first t of lo .. hi - 1 whose running sum is over x; the last one of weight above 0 if none is (the border was
-  // lost to the order of the sums), -1 without such a one.
-  __device__ __forceinline__ int64_t find(int64_t lo, int64_t hi, double x, double* s_red, int* s_last) const {
+  // The first t of lo .. hi - 1 of weight above 0 whose running sum is over x; the last one of weight above 0 if none is
+  // (the border was lost to the order of the sums), -1 without such a one.  By kDrawThreads threads.
+  __device__ __forceinline__ int64_t find(int64_t lo, int64_t hi, double x, double* s_red, int* s_at) const {
     constexpr int N = Elem<T>::kPerVec;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     double before = 0;
     int64_t last = -1;
-    for (int64_t t0 = lo; t0 < hi; t0 += kThreads * N) {
+    for (int64_t t0 = lo; t0 < hi; t0 += kDrawThreads * N) {
       const int64_t t = t0 + threadIdx.x * N;
       double w[N], sum = 0;
       int mine = -1;
@@ -97,41 +112,42 @@ struct Row {
           if (w[i] > 0) mine = i;
         }
       }
-      double upto = sum;
-#pragma unroll
-      for (int d = 1; d < 64; d <<= 1) {
-        const double o = __shfl_up(upto, d, 64);
-        if (lane >= d) upto += o;
-      }
-      __syncthreads();
+      const double upto = scan(sum);
       if (lane == 63) s_red[wave] = upto;
-      if (threadIdx.x < kWaves) s_last[threadIdx.x] = s_last[kWaves + threadIdx.x] = -1;
+      const uint64_t some = __builtin_amdgcn_ballot_w64(mine >= 0);
+      const int back = some != 0 ? 63 - __clzll((unsigned long long)some) : -1;  // the last lane with some weight
+      if (lane == max(back, 0)) s_at[kMostWaves + wave] = back < 0 ? -1 : (int)threadIdx.x * N + mine;
+      if (lane == 0) s_at[wave] = -1;
       __syncthreads();
       double base = before;
       for (int i = 0; i < wave; ++i) base += s_red[i];
-      // (only lanes with some weight: a token without any is never drawn, whatever the sums' roundings)
-      const uint64_t some = __builtin_amdgcn_ballot_w64(mine >= 0);
-      const uint64_t over = __builtin_amdgcn_ballot_w64(mine >= 0 && base + upto > x);
-      if (over != 0 && lane == __ffsll((unsigned long long)over) - 1) {
-        double run = base + upto - sum;
-        int at = -1;
+      // the wavefront that the border lies in, and there the first lane with weight that is past it
+      if (base <= x && base + s_red[wave] > x) {
+        const uint64_t over = some & __builtin_amdgcn_ballot_w64(base + upto > x);
+        const int front = over != 0 ? __ffsll((unsigned long long)over) - 1 : back;
+        if (lane == front) {
+          double run = base + (upto - sum);
+          int at = mine;
+          for (int i = N - 1; i >= 0; --i) {
+            double r = run;
 #pragma unroll
-        for (int i = N - 1; i >= 0; --i) {
-          double r = run;
+            for (int j = 0; j < N; ++j) r += j <= i ? w[j] : 0.0;
+            bool weighs = false;
 #pragma unroll
-          for (int j = 0; j <= i; ++j) r += w[j];
-          if (r > x && w[i] > 0) at = i;
+            for (int j = 0; j < N; ++j) weighs |= j == i && w[j] > 0;
+            if (weighs && r > x) at = i;
+          }
+          s_at[wave] = threadIdx.x * N + at;
         }
-        s_last[wave] = (at < 0 ? mine : at) + threadIdx.x * N;
       }
-      if (some != 0 && lane == 63 - __clzll((unsigned long long)some)) s_last[kWaves + wave] = mine + threadIdx.x * N;
       __syncthreads();
-      for (int i = 0; i < kWaves; ++i)
-        if (s_last[i] >= 0) return t0 + s_last[i];
-      for (int i = 0; i < kWaves; ++i) {
-        if (s_last[kWaves + i] >= 0) last = t0 + s_last[kWaves + i];
+      for (int i = 0; i < kMostWaves; ++i)
+        if (s_at[i] >= 0) return t0 + s_at[i];
+      for (int i = 0; i < kMostWaves; ++i) {
+        if (s_at[kMostWaves + i] >= 0) last = t0 + s_at[kMostWaves + i];
         before += s_red[i];
       }
+      __syncthreads();
     }
     return last;
   }
@@ -141,14 +157,19 @@ struct Place {
   int row0, n, accepted;  // rows of the sequence; drafts: n - 1
 };
 
-// The sequence's rows and how many of its drafts are accepted: 64 drafts at a time, by every wavefront.
-template <typename T>
-__device__ __forceinline__ Place place_of(const VerifyDrafts& a, int b) {
+__device__ __forceinline__ Place rows_of(const VerifyDrafts& a, int b) {
   Place w;
   const int s0 = a.seq_start[b], s1 = a.seq_start[b + 1];
   w.row0 = min(max(s0, 0), a.R);
   w.n = min(max(s1, w.row0), a.R) - w.row0;
   w.accepted = max(0, w.n - 1);
+  return w;
+}
+
+// The sequence's rows and how many of its drafts are accepted: 64 drafts at a time, by every wavefront.
+template <typename T>
+__device__ __forceinline__ Place place_of(const VerifyDrafts& a, int b) {
+  Place w = rows_of(a, b);
   const int lane = threadIdx.x & 63;
   for (int i0 = 0; i0 < w.n - 1; i0 += 64) {
     const int i = i0 + lane;
@@ -184,70 +205,80 @@ __device__ __forceinline__ Row<T> row_of(const VerifyDrafts& a, const Place& w, 
   return row;
 }
 
-// values of a slice: whole turns of the workgroup, so that a slice's first vector is a thread's first
-__host__ __device__ inline int64_t slice_values(int64_t V, int per_turn) {
+// Values of a slice: whole turns of a summing workgroup, so that every slice starts at the same place of a vector.  A
+// workgroup makes three trips to memory before its first value, so that it should have some thousand values, but not
+// many thousands (us, both launches, fp32, slices of 8192 / 4096 / 2048 values: 64 x 131072 20.9 / 18.3 / 18.4, 128 x
+// 131072 29.6 / 26.5 / -; bf16, 128 x 50001 13.4 / 12.1 / 13.0); where few workgroups come of it, half as many.
+inline int64_t slice_values(int64_t B, int64_t V, int per_turn) {
+  int64_t v = B * ((V + 4095) / 4096) >= 256 ? 4096 : 2048;
   const int64_t least = (V + kSlices - 1) / kSlices;
-  const int64_t v = least > kLeastSlice ? least : kLeastSlice;
+  v = least > v ? least : v;
   return (v + per_turn - 1) / per_turn * per_turn;
 }
 
+// sums: [B][slices], then how many drafts each sequence has accepted, [B] of 32 bits.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void verify_sums_kernel(const VerifyDrafts a, double* sums, int slices, int64_t values) {
-  __shared__ double s_red[kWaves];
-  const int b = blockIdx.x / slices, s = blockIdx.x - b * slices;
+__global__ __launch_bounds__(kSumThreads) void verify_sums_kernel(const VerifyDrafts a, double* sums, int slices, int64_t values) {
+  __shared__ double s_red[kSumThreads / kWave];
+  const int b = (unsigned)blockIdx.x / (unsigned)slices, s = blockIdx.x - b * slices;
   const Place w = place_of<T>(a, b);
   if (w.n == 0) return;
   const Row<T> row = row_of<T>(a, w, false);
   const int64_t lo = s * values;
-  const double sum = row.slice_sum(lo, min(a.V, lo + values), s_red);
-  if (threadIdx.x == 0) sums[(int64_t)b * slices + s] = sum;
+  const double sum = row.template slice_sum<kSumThreads>(lo, min(a.V, lo + values), s_red);
+  if (threadIdx.x == 0) {
+    sums[(int64_t)b * slices + s] = sum;
+    if (s == 0) reinterpret_cast<int32_t*>(sums + (int64_t)a.B * slices)[b] = w.accepted;
+  }
 }
 
-// sums null: formed here.
+// sums null: all is found here.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void verify_draw_kernel(const VerifyDrafts a, const double* sums, int slices, int64_t values) {
-  __shared__ double s_red[kWaves], s_sums[kSlices];
-  __shared__ int s_last[2 * kWaves];
-  const int b = blockIdx.x;
-  const Place w = place_of<T>(a, b);
+__global__ __launch_bounds__(kDrawThreads) void verify_draw_kernel(const VerifyDrafts a, const double* sums, int slices, int64_t values) {
+  __shared__ double s_red[kMostWaves], s_sums[kSlices];
+  __shared__ int s_at[2 * kMostWaves];
+  const int b = blockIdx.x, lane = threadIdx.x & 63;
+  const double drawn = (double)a.u_sample[b];
+  Place w;
+  double mine = 0;  // a slice's sum, to each lane
+  if (sums != nullptr) {
+    mine = lane < slices ? sums[(int64_t)b * slices + lane] : 0.0;
+    const int accepted = reinterpret_cast<const int32_t*>(sums + (int64_t)a.B * slices)[b];
+    w = rows_of(a, b);
+    w.accepted = w.n > 0 ? accepted : 0;
+  } else {
+    w = place_of<T>(a, b);
+  }
   if (threadIdx.x == 0) a.accepted[b] = w.accepted;
   if (w.n == 0) return;
   Row<T> row = row_of<T>(a, w, false);
-  double total = 0;
-  for (int turn = 0; turn < 2; ++turn) {
-    if (sums != nullptr && turn == 0) {
-      if (threadIdx.x < slices) s_sums[threadIdx.x] = sums[(int64_t)b * slices + threadIdx.x];
-    } else {
+  double upto, total;
+  for (int turn = 0;; ++turn) {
+    if (sums == nullptr || turn != 0) {
       for (int s = 0; s < slices; ++s) {
         const int64_t lo = s * values;
-        const double v = row.slice_sum(lo, min(a.V, lo + values), s_red);
+        const double v = row.template slice_sum<kDrawThreads>(lo, min(a.V, lo + values), s_red);
         if (threadIdx.x == 0) s_sums[s] = v;
       }
+      __syncthreads();
+      mine = lane < slices ? s_sums[lane] : 0.0;
     }
-    __syncthreads();
-    total = 0;
-    for (int s = 0; s < slices; ++s) total += s_sums[s];
-    if (total != 0 || w.accepted == w.n - 1) break;
+    upto = scan(mine);
+    total = __shfl(upto, 63, 64);
+    if (total != 0 || w.accepted == w.n - 1 || turn != 0) break;
     row = row_of<T>(a, w, true);  // nothing is left of the target: its own probabilities
-    __syncthreads();
   }
   int64_t token = -1;
   if (total > 0 && total <= 1.7976931348623157e308) {
-    const double x = fmax((double)a.u_sample[b] * total, 0.0);
-    double upto = 0, before = 0;
-    int s = 0;
-    for (int i = 0; i < slices; ++i) {
-      if (s_sums[i] > 0) {  // (x at or past the total: the last slice that has any)
-        s = i;
-        before = upto;
-      }
-      upto += s_sums[i];
-      if (s_sums[i] > 0 && upto > x) break;
-    }
+    const double x = fmax(drawn * total, 0.0);
+    const uint64_t some = __builtin_amdgcn_ballot_w64(mine > 0), over = some & __builtin_amdgcn_ballot_w64(upto > x);
+    // (x at or past the total: the last slice that has any)
+    const int s = over != 0 ? __ffsll((unsigned long long)over) - 1 : 63 - __clzll((unsigned long long)some);
+    const double before = s > 0 ? __shfl(upto, max(s - 1, 0), 64) : 0.0;
     const int64_t lo = s * values;
-    token = row.find(lo, min(a.V, lo + values), x - before, s_red, s_last);
+    token = row.find(lo, min(a.V, lo + values), x - before, s_red, s_at);
   }
-  for (int i = threadIdx.x; i < w.n; i += kThreads)
+  for (int i = threadIdx.x; i < w.n; i += kDrawThreads)
     a.out[w.row0 + i] = i < w.accepted ? a.tokens[w.row0 + i] : i == w.accepted ? (int32_t)token : -1;
 }
 
@@ -256,19 +287,19 @@ int num_slices(int64_t V, int64_t values) { return (int)((V + values - 1) / valu
 }  // namespace
 
 size_t verify_drafts_bytes(int64_t B, int64_t V) {
-  const int slices = num_slices(V, slice_values(V, kThreads * 4));  // (rows of 4-byte values have as many slices or more)
-  return slices > 1 ? (size_t)B * slices * sizeof(double) : 0;
+  const int slices = num_slices(V, slice_values(B, V, kSumThreads * 4));  // (rows of 4-byte values have as many slices or more)
+  return slices > 1 ? ((size_t)B * slices * sizeof(double) + (size_t)B * sizeof(int32_t) + 15) & ~(size_t)15 : 0;
 }
 
 hipError_t launch_verify_drafts(const VerifyDrafts& a, void* workspace, hipStream_t s) {
-  const int64_t values = slice_values(a.V, kThreads * (a.bf16 ? 8 : 4));
+  const int64_t values = slice_values(a.B, a.V, kSumThreads * (a.bf16 ? 8 : 4));
   const int slices = num_slices(a.V, values);
   double* sums = slices > 1 ? (double*)workspace : nullptr;
-  if ((int64_t)a.B * slices > UINT32_MAX / kThreads) return hipErrorInvalidValue;
+  if ((int64_t)a.B * slices > UINT32_MAX / kSumThreads || a.B > UINT32_MAX / kDrawThreads) return hipErrorInvalidValue;
 #define RF_VERIFY(T)                                                                                                    \
   if (sums != nullptr)                                                                                                  \
-    hipLaunchKernelGGL((verify_sums_kernel<T>), dim3((unsigned)(a.B * slices)), dim3(kThreads), 0, s, a, sums, slices, values); \
-  hipLaunchKernelGGL((verify_draw_kernel<T>), dim3((unsigned)a.B), dim3(kThreads), 0, s, a, sums, slices, values)
+    hipLaunchKernelGGL((verify_sums_kernel<T>), dim3((unsigned)(a.B * slices)), dim3(kSumThreads), 0, s, a, sums, slices, values); \
+  hipLaunchKernelGGL((verify_draw_kernel<T>), dim3((unsigned)a.B), dim3(kDrawThreads), 0, s, a, sums, slices, values)
   if (a.bf16) {
     RF_VERIFY(bf16_t);
   } else {
