@@ -30,7 +30,7 @@ struct PagedArgs {
 // Writes the entry of the share's tile (or, where the batch has no such share, of one of the tiles that it does not
 // have either).  One wavefront of the workgroups of KV head 0 calls it.
 __device__ __forceinline__ void note_tile(const PagedArgs& a, int unit, bool found, const Share& w) {
-  if (a.deal.target == 0 || (threadIdx.x & 63) != 0) return;
+  if (a.deal.round == 0 || (threadIdx.x & 63) != 0) return;
   if (found) {
     const int R = 1 << a.deal.rows_log2, r0 = w.tile << a.deal.rows_log2;
     if (w.chunk == 0)

@@ -53,10 +53,23 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void paged_rows_kernel(const Page
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int i16 = lane & 15, g = lane >> 4;
 
-  const int unit = __builtin_amdgcn_readfirstlane(blockIdx.x / p.Hkv);
-  const int hk = __builtin_amdgcn_readfirstlane(blockIdx.x - unit * p.Hkv);
+  // Workgroups are dealt round-robin to the 8 XCDs: the KV heads of a share go to one of them, one behind the other.
+  // Their rows lie side by side in memory, and the XCD's address translation and page table lookups serve all of them.
+  // Workgroups are dealt round-robin to the 8 XCDs.  Rows of up to 128 bytes: the KV heads of a share go to one of them,
+  // one behind the other, so that its address translation serves neighbouring heads' rows together (32 contexts of 32768
+  // in FP8, d = 128, 425 -> 402 us); longer rows gain nothing by it (64 contexts of 4300 in bf16 207 -> 213).
+  int unit, hk;
+  if constexpr (kRow <= 128) {
+    const int turn = __builtin_amdgcn_readfirstlane((blockIdx.x >> 3) / (unsigned)p.Hkv);
+    hk = __builtin_amdgcn_readfirstlane((blockIdx.x >> 3) - turn * p.Hkv);
+    unit = turn * 8 + (blockIdx.x & 7);
+  } else {
+    unit = __builtin_amdgcn_readfirstlane(blockIdx.x / (unsigned)p.Hkv);
+    hk = __builtin_amdgcn_readfirstlane(blockIdx.x - unit * p.Hkv);
+  }
   Share w;
-  const bool found = find_share(p, a.deal, unit, &w);
+  __shared__ ShareScratch s_share;
+  const bool found = find_share(p, a.deal, unit, &s_share, &w);
   if (hk == 0 && wave == 0) note_tile(a, unit, found, w);
   if (!found) return;
 
@@ -112,13 +125,13 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void paged_rows_kernel(const Page
 #pragma unroll
     for (int e = 0; e < kLoads; ++e) {
       const int f = e * kRpl / 16, row = e * kRpl % 16;
-      kreg[e] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(a.k + base[f] + (k_lane + row * slot_bytes)));
+      kreg[e] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(a.k + (base[f] + (int64_t)(row * slot_bytes)) + k_lane));
     }
   };
   auto issue_v = [&](const int64_t (&base)[2], uint32_t (&vreg)[8][VL]) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const unsigned char* at = a.v + base[e >> 2] + (v_lane + (e & 3) * slot_bytes);
+      const unsigned char* at = a.v + (base[e >> 2] + (int64_t)((e & 3) * slot_bytes)) + v_lane;
       if constexpr (VL == 4) {
         const u32x4 t = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(at));
 #pragma unroll
@@ -146,16 +159,28 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void paged_rows_kernel(const Page
   unsigned char* ktile = smem + wave * kTile;
   auto k_slot = [&](int row, int piece) { return ktile + row * kLdsRow + ((piece ^ (row & (kSlots - 1))) << 4); };
 
-  // D[d][row] of V^T P^T for all of a step's keys
-  auto product = [&](const uint32_t (&vb)[8][VW], const u32x4& pb, int tp, f32x4& even, f32x4& odd) {
+  // O^T += V^T P^T for the values 2 tp, 2 tp + 1 of each lane's V rows (a 2 x 8 transpose of 16-bit values in registers)
+  auto product = [&](const uint32_t (&vr)[8][VL], const u32x4 (&pb)[NR], int tp) __attribute__((always_inline)) {
     u32x4 lo4, hi4;
 #pragma unroll
     for (int ep = 0; ep < 4; ++ep) {
-      lo4[ep] = pair_lo(vb[2 * ep][tp], vb[2 * ep + 1][tp]);
-      hi4[ep] = pair_hi(vb[2 * ep][tp], vb[2 * ep + 1][tp]);
+      uint32_t x, y;
+      if constexpr (FP8) {
+        x = (tp & 1) ? fp8_hi_to_bf16(vr[2 * ep][tp >> 1]) : fp8_lo_to_bf16(vr[2 * ep][tp >> 1]);
+        y = (tp & 1) ? fp8_hi_to_bf16(vr[2 * ep + 1][tp >> 1]) : fp8_lo_to_bf16(vr[2 * ep + 1][tp >> 1]);
+      } else {
+        x = vr[2 * ep][tp];
+        y = vr[2 * ep + 1][tp];
+      }
+      lo4[ep] = pair_lo(x, y);
+      hi4[ep] = pair_hi(x, y);
     }
-    even = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, lo4), __builtin_bit_cast(bf16x8, pb), even, 0, 0, 0);
-    odd = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, hi4), __builtin_bit_cast(bf16x8, pb), odd, 0, 0, 0);
+#pragma unroll
+    for (int nr = 0; nr < NR; ++nr) {
+      f32x4 &even = acc[nr][2 * tp], &odd = acc[nr][2 * tp + 1];
+      even = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, lo4), __builtin_bit_cast(bf16x8, pb[nr]), even, 0, 0, 0);
+      odd = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, hi4), __builtin_bit_cast(bf16x8, pb[nr]), odd, 0, 0, 0);
+    }
   };
 
   int64_t base[2];
@@ -166,6 +191,7 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void paged_rows_kernel(const Page
     base[1] = half_base(at, 1);
     ++at;
   };
+  uint64_t odd_keys = 0;  // bit j: key seen_all + j (a tile's rows differ by less than 32 keys)
   u32x4 kreg[kLoads];
   uint32_t vreg[8][VL];
   int key0 = lo + wave * kStepKeys;
@@ -178,9 +204,13 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void paged_rows_kernel(const Page
   for (; key0 < hi; key0 += kChunkStep) {
     const bool more = key0 + kChunkStep < hi;
     // ---- K: registers -> this wavefront's LDS, as bf16 ----
+    // (opaque copies of the lane's number here and below: addresses made of them are made here, and not ahead of the loop
+    // to be carried through it in registers)
+    int ln = lane;
+    asm volatile("" : "+v"(ln));
 #pragma unroll
     for (int e = 0; e < kLoads; ++e) {
-      const int row = e * kRpl + lane / kLpr, c = lane % kLpr;
+      const int row = e * kRpl + ln / kLpr, c = ln % kLpr;
       if constexpr (FP8) {
         u32x4 w0, w1;
 #pragma unroll
@@ -212,7 +242,7 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void paged_rows_kernel(const Page
     for (int kk = 0; kk < KS; ++kk)
 #pragma unroll
       for (int f = 0; f < 2; ++f) {
-        const u32x4 ka = *reinterpret_cast<const u32x4*>(k_slot(16 * f + i16, 4 * kk + g));
+        const u32x4 ka = *reinterpret_cast<const u32x4*>(k_slot(16 * f + (ln & 15), 4 * kk + (ln >> 4)));
 #pragma unroll
         for (int nr = 0; nr < NR; ++nr)
           s[nr][f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ka),
@@ -251,60 +281,48 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void paged_rows_kernel(const Page
     }
 
     // ---- acc += V^T P^T ----
-    uint32_t vb[8][VW];
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-#pragma unroll
-      for (int i = 0; i < VW; ++i) {
-        if constexpr (FP8) vb[e][i] = (i & 1) ? fp8_hi_to_bf16(vreg[e][i >> 1]) : fp8_lo_to_bf16(vreg[e][i >> 1]);
-        else vb[e][i] = vreg[e][i];
-      }
     if (key0 + kStepKeys > seen_all) {
-      // Keys that some rows do not see, or none.  Their probabilities are 0 there, but 0 times infinity or NaN is not:
-      // what no row sees (slots behind the last token among it) is taken out, and where a value that some rows see is
-      // not finite, the keys from the first such one on go one by one, to the rows that see them.
-      uint32_t odd = 0;
+      // Keys that some rows do not see, or none, have probability 0 there, but 0 times infinity or NaN is not 0.  What no
+      // row sees (slots behind the last token among it) is cleared, and values of the others that are not finite are
+      // cleared and their keys noted: once the keys are done they are added to the rows that see them (a probability is
+      // above 0 by definition, so the value itself will do).
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const int key = key0 + 4 * g + ((e < 4) ? e : 12 + e);
+        uint32_t odd = 0;
 #pragma unroll
-        for (int i = 0; i < VW; ++i) {
-          vb[e][i] = key < hi ? vb[e][i] : 0u;
-          odd |= key >= seen_all ? not_finite(vb[e][i]) : 0u;
+        for (int i = 0; i < VL; ++i) {
+          const uint32_t f = key >= seen_all ? not_finite<FP8>(vreg[e][i]) : 0u;
+          odd |= f;
+          vreg[e][i] = key < hi ? vreg[e][i] & ~f : 0u;
         }
-      }
-      if (__builtin_amdgcn_ballot_w64(odd != 0) != 0) {
-        const int from = max(seen_all, key0), to = min(hi, key0 + kStepKeys);
-        for (int one = from; one < to; ++one) {
+        const uint64_t noted = __builtin_amdgcn_ballot_w64(odd != 0 && key < hi);
+        if (noted != 0) {
 #pragma unroll
-          for (int tp = 0; tp < VW; ++tp) {
-            uint32_t vo[8][VW];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) vo[e][tp] = key0 + 4 * g + ((e < 4) ? e : 12 + e) == one ? vb[e][tp] : 0u;
-#pragma unroll
-            for (int nr = 0; nr < NR; ++nr) {
-              f32x4 even = {0.f, 0.f, 0.f, 0.f}, od = even;
-              product(vo, pb[nr], tp, even, od);
-              const bool see = one < seen[nr];
-#pragma unroll
-              for (int rr = 0; rr < 4; ++rr) {
-                acc[nr][2 * tp][rr] += see ? even[rr] : 0.f;
-                acc[nr][2 * tp + 1][rr] += see ? od[rr] : 0.f;
-              }
-            }
-          }
+          for (int gg = 0; gg < 4; ++gg)
+            if ((noted >> (16 * gg) & 0xffff) != 0) odd_keys |= 1ull << (key0 + 4 * gg + ((e < 4) ? e : 12 + e) - seen_all);
         }
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-#pragma unroll
-          for (int i = 0; i < VW; ++i) vb[e][i] = key0 + 4 * g + ((e < 4) ? e : 12 + e) < seen_all ? vb[e][i] : 0u;
       }
     }
 #pragma unroll
-    for (int tp = 0; tp < VW; ++tp)
-#pragma unroll
-      for (int nr = 0; nr < NR; ++nr) product(vb, pb[nr], tp, acc[nr][2 * tp], acc[nr][2 * tp + 1]);
+    for (int tp = 0; tp < VW; ++tp) product(vreg, pb, tp);
     if (more) issue_v(base, vreg);
+  }
+
+  for (; odd_keys != 0; odd_keys &= odd_keys - 1) {
+    const int key = seen_all + __builtin_ctzll(odd_keys), in = (unsigned)key / (unsigned)p.page;
+    int id = p.pages[(int64_t)w.b * p.table_pitch + in];
+    id = id < 0 || id >= p.n_pages ? 0 : id;
+    const int64_t off = (int64_t)id * p.page_stride + (int64_t)(key - in * p.page) * p.slot_stride + (int64_t)hk * p.head_stride;
+#pragma unroll
+    for (int rr = 0; rr < 4; ++rr)
+#pragma unroll
+      for (int t = 0; t < DPL; ++t) {
+        const uint32_t x = cached_bf16<FP8>(a.v, off + DPL * (4 * g + rr) + t);
+        const float y = not_finite<false>(x) != 0 ? from_bf16((bf16_t)x) : 0.f;
+#pragma unroll
+        for (int nr = 0; nr < NR; ++nr) acc[nr][t][rr] += key < seen[nr] ? y : 0.f;
+      }
   }
 
   // ---- merge of the four wavefronts' states, 16 rows at a time ----
@@ -370,7 +388,7 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void paged_rows_kernel(const Page
 }  // namespace
 
 hipError_t launch_paged_rows(const PagedArgs& a, bool fp8, hipStream_t s) {
-  const int64_t grid = ((int64_t)a.n_tiles + a.deal.target) * a.p.Hkv;
+  const int64_t grid = ((int64_t)a.n_tiles + a.deal.target() + 7) / 8 * 8 * a.p.Hkv;  // (of whole turns over the XCDs)
   if (grid > UINT32_MAX / (kWaves * kWave)) return hipErrorInvalidValue;
 #define RF_ROWS(DD, NN, F8) \
   hipLaunchKernelGGL((paged_rows_kernel<DD, NN, F8>), dim3((unsigned)grid), dim3(kWaves * kWave), 0, s, a)

@@ -66,7 +66,8 @@ __global__ __launch_bounds__(kNW* kWave, 2) void paged_tiles_kernel(const PagedA
   const int hk = __builtin_amdgcn_readfirstlane(blockIdx.x - block * p.Hkv);
   const int unit = n_units - 1 - block;
   Share w;
-  const bool found = find_share(p, a.deal, unit, &w);
+  __shared__ ShareScratch s_share;
+  const bool found = find_share(p, a.deal, unit, &s_share, &w);
   if (hk == 0 && wave == 0) note_tile(a, unit, found, w);
   if (!found) return;
 
@@ -391,10 +392,9 @@ __global__ __launch_bounds__(kNW* kWave, 2) void paged_tiles_kernel(const PagedA
       uint32_t odd = 0;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const uint32_t f = not_finite(x[i]);
+        const uint32_t f = not_finite<false>(x[i]);
         odd |= f;
-        x[i] &= ~(((f >> 15) & 1) * 0xffffu | (f >> 31) * 0xffff0000u);
-        x[i] = key <= wg_last ? x[i] : 0u;
+        x[i] = key <= wg_last ? x[i] & ~f : 0u;
       }
       if (key > wg_last || (key > wg_min_last && odd != 0)) *at = x;
       if (key > wg_min_last && key <= wg_last && odd != 0) atomicOr(&s_noted[(key - edge0) >> 5], 1u << ((key - edge0) & 31));
@@ -441,7 +441,7 @@ __global__ __launch_bounds__(kNW* kWave, 2) void paged_tiles_kernel(const PagedA
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const uint32_t x = cached_bf16<FP8>(a.v, off + 32 * t + 8 * (r >> 2) + 4 * hh + (r & 3));
-          const bool take = (key <= my_last) & (not_finite(x) != 0);
+          const bool take = (key <= my_last) & (not_finite<false>(x) != 0);
           acc[t][r] += take ? from_bf16((bf16_t)x) : 0.f;
         }
     }
@@ -518,7 +518,7 @@ __global__ __launch_bounds__(kNW* kWave, 2) void paged_tiles_kernel(const PagedA
 }  // namespace
 
 hipError_t launch_paged_tiles(const PagedArgs& a, bool fp8, hipStream_t s) {
-  const int64_t units = (int64_t)a.n_tiles + a.deal.target, grid = units * a.p.Hkv;
+  const int64_t units = (int64_t)a.n_tiles + a.deal.target(), grid = units * a.p.Hkv;
   if (grid > UINT32_MAX / (kNW * kWave)) return hipErrorInvalidValue;
 #define RF_TILES(DD, F8) \
   hipLaunchKernelGGL((paged_tiles_kernel<DD, F8>), dim3((unsigned)grid), dim3(kNW * kWave), 0, s, a, (int)units)

@@ -59,14 +59,18 @@ __device__ __forceinline__ int wave_inclusive_scan(int v) {
 }
 
 // How a launch of the attention kernels deals out a ragged batch.  The sequences whose packed rows (new tokens times
-// query heads that share a KV head) number lo_rows + 1 .. hi_rows belong to the launch, 1 << rows_log2 of them make a tile,
-// and a tile's keys are cut into chunks of one length.  That length follows from the keys of the whole batch, so that
-// about `target` chunks of equal size come out however unequal the sequences are: the host, which does not know the
-// lengths, need not.  (target 0: one chunk a tile.)
+// query heads that share a KV head) number lo_rows + 1 .. hi_rows belong to the launch, 1 << rows_log2 of them make a
+// tile, and a tile's keys are cut into chunks of one length.  That length follows from the keys of the whole batch, so
+// that chunks of equal size come out however unequal the sequences are: the host, which does not know the lengths, need
+// not.
 struct Deal {
   int rows_log2, lo_rows, hi_rows;
-  int target, least;  // least: keys of the smallest chunk, a multiple of 128
+  int round;   // shares that the chip takes at once, for one KV head; 0: nothing is cut
+  int rounds;  // of the chunks of long contexts
+  __host__ __device__ int target() const { return round * rounds; }
 };
+constexpr int kLeastChunk = 128;   // keys
+constexpr int kLongShare = 32;     // of 64 keys each: a workgroup's in one round, from which on a context is long
 
 struct Share {
   Sequence s;
@@ -76,71 +80,202 @@ struct Share {
   int all_shares, all_tiles;  // of the batch (where there is no such share)
 };
 
-// Share number `unit` of the batch; false past the last one.  Shares
-// are counted sequence by sequence, tile by tile.  There are at most target + tiles of them, and at most 2 target with
-// more than one chunk to their tile: such a tile has over chunk_keys keys, so ceil(keys / chunk_keys) is below twice
-// keys / chunk_keys, and the sum of all keys / chunk_keys is at most target.
-__device__ __forceinline__ bool find_share(const Paged& p, const Deal& d, int unit, Share* out) {
+// Keys of a chunk, a multiple of 128, or INT32_MAX: from the tiles of the batch, the keys that they have together and
+// the longest one's, these in units of 64 (so that 32 bits hold the sum).
+//  - A batch whose longest tile is little more than a workgroup's share of one round is not cut.
+//  - Little work goes in one round: a second one would cost a workgroup's way into the cache (the arrays, the page
+//    table, the first keys: three trips to memory) again.  Every sequence's last chunk is half empty on average.
+//  - Much goes in several, so that unequal last chunks do not leave the chip idle at the end.
+// us of a decode step, 32 heads over 8, d = 128, with chunks for one round / two / four: 64 contexts of 400 to 8192
+// 229 / 210 / 203; one of 32768 34 / 40 / 43; 8 of 2000 19 / 20 / 21.
+__device__ __forceinline__ int chunk_keys_of(const Deal& d, unsigned tiles, unsigned units, unsigned longest) {
+  if (d.round == 0) return INT32_MAX;
+  const unsigned even = (units + d.round - 1) / (unsigned)d.round;
+  if (longest <= even + even / 8) return INT32_MAX;
+  unsigned share;
+  if (even <= kLongShare) {
+    const unsigned left = tiles < (unsigned)d.round ? d.round - tiles / 2 : d.round;
+    share = (units + left - 1) / left;
+  } else {
+    share = (units + d.target() - 1) / (unsigned)d.target();
+  }
+  return (int)min(((uint64_t)share * 64 + 127) & ~(uint64_t)127, (uint64_t)(INT32_MAX - 127));
+}
+
+__device__ __forceinline__ unsigned chunks_of(int len, int chunk_keys) {
+  return len <= chunk_keys ? 1u : ((unsigned)len + (unsigned)chunk_keys - 1) / (unsigned)chunk_keys;
+}
+
+__device__ __forceinline__ int tiles_of(const Paged& p, const Deal& d, const Sequence& s) {
+  const int rows = s.n * p.group;
+  return rows > d.lo_rows && rows <= d.hi_rows ? ((rows - 1) >> d.rows_log2) + 1 : 0;
+}
+
+// What find_share needs of LDS.
+struct ShareScratch {
+  int totals[4][4];
+  Share share;
+  int found;
+};
+
+// Share number `unit` of the batch; false past the last one.  Shares are counted sequence by sequence, tile by tile.
+// There are at most target + tiles of them, and at most 2 target with more than one chunk to their tile: such a tile has
+// over chunk_keys keys, so ceil(keys / chunk_keys) is below twice keys / chunk_keys, and the sum of all keys / chunk_keys
+// is at most target.  Called by whole workgroups of 256 threads.
+__device__ __forceinline__ bool find_share(const Paged& p, const Deal& d, int unit, ShareScratch* scratch, Share* out) {
   const int lane = threadIdx.x & 63;
-  auto load = [&](int b0, int* tiles) {
+  auto units_of = [](const Sequence& x) { return (unsigned)(x.len + 63) >> 6; };
+  if (p.B <= kWave) {
+    // a sequence to a lane, in every wavefront
     Sequence s{0, 0, 0, false};
-    *tiles = 0;
-    if (b0 + lane < p.B) {
-      s = load_sequence(p, b0 + lane);
-      const int rows = s.n * p.group;
-      if (rows > d.lo_rows && rows <= d.hi_rows) *tiles = ((rows - 1) >> d.rows_log2) + 1;
+    if (lane < p.B) s = load_sequence(p, lane);
+    const int tiles = tiles_of(p, d, s);
+    const int tiles_upto = wave_inclusive_scan(tiles), all_tiles = __builtin_amdgcn_readlane(tiles_upto, 63);
+    int chunk_keys = INT32_MAX;
+    if (d.round > 0) {
+      const unsigned units = __builtin_amdgcn_readlane(wave_inclusive_scan(tiles * units_of(s)), 63);
+      // (exact below 2^24; sequences beyond are cut anyway)
+      const unsigned longest = (unsigned)wave_max(tiles > 0 ? (float)units_of(s) : 0.f);
+      chunk_keys = __builtin_amdgcn_readfirstlane(chunk_keys_of(d, all_tiles, units, longest));
     }
-    return s;
+    const int chunks = chunks_of(s.len, chunk_keys);
+    const int upto = wave_inclusive_scan(tiles * chunks), slots_upto = wave_inclusive_scan(chunks > 1 ? tiles * chunks : 0);
+    const uint64_t past = __builtin_amdgcn_ballot_w64(upto > unit);
+    if (past == 0) {
+      out->all_shares = __builtin_amdgcn_readlane(upto, 63);
+      out->all_tiles = all_tiles;
+      return false;
+    }
+    const int f = __ffsll((unsigned long long)past) - 1;
+    auto get = [&](int v) { return __builtin_amdgcn_readlane(v, f); };
+    out->chunks = get(chunks);
+    const int units = get(tiles) * out->chunks, at = unit - (get(upto) - units);
+    out->tile = out->chunks == 1 ? at : __builtin_amdgcn_readfirstlane((unsigned)at / (unsigned)out->chunks);
+    out->chunk = at - out->tile * out->chunks;
+    out->slot = get(slots_upto) - units + at;
+    out->tile_index = get(tiles_upto) - get(tiles) + out->tile;
+    out->b = f;
+    out->chunk_keys = chunk_keys;
+    out->s = Sequence{get(s.row0), get(s.n), get(s.len), get((int)s.over) != 0};
+    return true;
+  }
+  // four sequences to a thread, 1024 at a time
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  constexpr int kEach = 4, kBlock = 4 * kWave * kEach;
+  Sequence s[kEach];
+  int tiles[kEach];
+  auto load = [&](int b0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int b = b0 + threadIdx.x * kEach + i;
+      s[i] = Sequence{0, 0, 0, false};
+      if (b < p.B) s[i] = load_sequence(p, b);
+      tiles[i] = tiles_of(p, d, s[i]);
+    }
   };
-  int tiles;
-  Sequence s = load(0, &tiles);
+  load(0);
   int chunk_keys = INT32_MAX;
-  if (d.target > 0) {
-    float keys = (float)tiles * (float)s.len;
-    for (int b0 = 64; b0 < p.B; b0 += 64) {
-      int t;
-      const Sequence x = load(b0, &t);
-      keys += (float)t * (float)x.len;
+  if (threadIdx.x == 0) scratch->found = 0;
+  if (d.round > 0) {
+    unsigned units = 0, longest = 0, all = 0;
+    for (int b0 = 0;;) {
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        units += tiles[i] * units_of(s[i]);
+        longest = max(longest, tiles[i] > 0 ? units_of(s[i]) : 0);
+        all += tiles[i];
+      }
+      b0 += kBlock;
+      if (b0 >= p.B) break;
+      load(b0);
     }
-    // (1.0001: at least what the sum in 32 bits may have lost)
-    const float share = fminf(ceilf(wave_sum(keys) / (float)d.target * 1.0001f), 2e9f);
-    chunk_keys = max(d.least, ((int)share + 127) & ~127);
+    units = wave_inclusive_scan(units);
+    all = wave_inclusive_scan(all);
+    longest = (unsigned)wave_max((float)longest);
+    if (lane == 63) {
+      scratch->totals[0][wave] = units;
+      scratch->totals[1][wave] = all;
+      scratch->totals[2][wave] = longest;
+    }
+    __syncthreads();
+    auto sum = [&](int k) { return (unsigned)(scratch->totals[k][0] + scratch->totals[k][1] + scratch->totals[k][2] + scratch->totals[k][3]); };
+    longest = max(max(scratch->totals[2][0], scratch->totals[2][1]), max(scratch->totals[2][2], scratch->totals[2][3]));
+    chunk_keys = __builtin_amdgcn_readfirstlane(chunk_keys_of(d, sum(1), sum(0), longest));
+    if (p.B > kBlock) load(0);
   }
   int base = 0, slot_base = 0, tile_base = 0;
   for (int b0 = 0;;) {
-    const int chunks = s.len <= chunk_keys ? 1 : (int)(((unsigned)s.len + chunk_keys - 1) / (unsigned)chunk_keys);
-    const int upto = wave_inclusive_scan(tiles * chunks);
-    const int slots_upto = wave_inclusive_scan(chunks > 1 ? tiles * chunks : 0);
-    const int tiles_upto = wave_inclusive_scan(tiles);
-    const uint64_t past = __builtin_amdgcn_ballot_w64(base + upto > unit);
-    if (past != 0) {
-      const int f = __ffsll((unsigned long long)past) - 1;
-      auto get = [&](int v) { return __builtin_amdgcn_readlane(v, f); };
-      out->chunks = get(chunks);
-      const int units = get(tiles) * out->chunks;
-      const int at = unit - (base + get(upto) - units);
-      out->tile = out->chunks == 1 ? at : __builtin_amdgcn_readfirstlane(at / out->chunks);
-      out->chunk = at - out->tile * out->chunks;
-      out->slot = slot_base + get(slots_upto) - units + at;
-      out->tile_index = tile_base + get(tiles_upto) - get(tiles) + out->tile;
-      out->b = b0 + f;
-      out->chunk_keys = __builtin_amdgcn_readfirstlane(chunk_keys);
-      out->s.row0 = get(s.row0);
-      out->s.n = get(s.n);
-      out->s.len = get(s.len);
-      out->s.over = get((int)s.over) != 0;
+    int mine = 0, slots = 0, here = 0, chunks[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      chunks[i] = chunks_of(s[i].len, chunk_keys);
+      mine += tiles[i] * chunks[i];
+      slots += chunks[i] > 1 ? tiles[i] * chunks[i] : 0;
+      here += tiles[i];
+    }
+    const int upto = wave_inclusive_scan(mine), slots_upto = wave_inclusive_scan(slots), here_upto = wave_inclusive_scan(here);
+    __syncthreads();  // the totals before have been read
+    if (lane == 63) {
+      scratch->totals[0][wave] = upto;
+      scratch->totals[1][wave] = slots_upto;
+      scratch->totals[2][wave] = here_upto;
+    }
+    __syncthreads();
+    int from = base + upto - mine, slot = slot_base + slots_upto - slots, tile = tile_base + here_upto - here;
+    for (int i = 0; i < 4; ++i) {
+      if (i < wave) {
+        from += scratch->totals[0][i];
+        slot += scratch->totals[1][i];
+        tile += scratch->totals[2][i];
+      }
+      base += scratch->totals[0][i];
+      slot_base += scratch->totals[1][i];
+      tile_base += scratch->totals[2][i];
+    }
+    if (unit >= from && unit < from + mine) {
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        const int units = tiles[i] * chunks[i];
+        if (unit >= from && unit < from + units) {
+          Share w;
+          w.s = s[i];
+          w.b = b0 + threadIdx.x * kEach + i;
+          w.tile = (unsigned)(unit - from) / (unsigned)chunks[i];
+          w.chunk = unit - from - w.tile * chunks[i];
+          w.chunks = chunks[i];
+          w.chunk_keys = chunk_keys;
+          w.slot = slot + unit - from;
+          w.tile_index = tile + w.tile;
+          w.all_shares = w.all_tiles = 0;
+          scratch->share = w;
+          scratch->found = 1;
+        }
+        from += units;
+        slot += chunks[i] > 1 ? units : 0;
+        tile += tiles[i];
+      }
+    }
+    __syncthreads();
+    if (scratch->found != 0) {
+      const Share w = scratch->share;
+      auto uniform = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+      out->s = Sequence{uniform(w.s.row0), uniform(w.s.n), uniform(w.s.len), uniform((int)w.s.over) != 0};
+      out->b = uniform(w.b);
+      out->tile = uniform(w.tile);
+      out->chunk = uniform(w.chunk);
+      out->chunks = uniform(w.chunks);
+      out->chunk_keys = uniform(w.chunk_keys);
+      out->slot = uniform(w.slot);
+      out->tile_index = uniform(w.tile_index);
       return true;
     }
-    base += __builtin_amdgcn_readlane(upto, 63);
-    slot_base += __builtin_amdgcn_readlane(slots_upto, 63);
-    tile_base += __builtin_amdgcn_readlane(tiles_upto, 63);
-    b0 += 64;
+    b0 += kBlock;
     if (b0 >= p.B) {
-      out->all_shares = base;
-      out->all_tiles = tile_base;
+      out->all_shares = __builtin_amdgcn_readfirstlane(base);
+      out->all_tiles = __builtin_amdgcn_readfirstlane(tile_base);
       return false;
     }
-    s = load(b0, &tiles);
+    load(b0);
   }
 }
 
@@ -152,8 +287,13 @@ __device__ __forceinline__ uint32_t fp8_hi_to_bf16(uint32_t w) {
   return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true));
 }
 
-// Nonzero where one of two packed bf16 values is an infinity or NaN (its exponent all ones).
-__device__ __forceinline__ uint32_t not_finite(uint32_t x) { return ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
+// All bits of the packed values (bf16, or FP8 E4M3) that are infinities or NaN: an exponent of all ones; all but the sign
+// set.
+template <bool FP8>
+__device__ __forceinline__ uint32_t not_finite(uint32_t x) {
+  if constexpr (FP8) return ((((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7) * 0xffu;
+  return ((((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u) >> 15) * 0xffffu;
+}
 
 // Element `at` of a cache as bf16.
 template <bool FP8>

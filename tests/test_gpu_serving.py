@@ -59,7 +59,11 @@ ATTENTION = [
     ([4, 0, 7], [2, 50, 3], 8, 8, 128, 16),                                # fewer keys than tokens: rows that see nothing
     ([17], [100], 1, 1, 64, 16), ([33], [1500], 2, 1, 128, 32), ([40, 1, 0, 9], [40, 900, 77, 300], 12, 4, 64, 80),
     ([130], [130], 4, 1, 128, 64), ([129, 1], [700, 64], 8, 2, 64, 16), ([300, 1, 1], [1100, 500, 2], 4, 2, 128, 16),
-    ([256], [2300], 8, 8, 64, 128), ([65], [64 * 20 + 1], 6, 2, 128, 48), ([700], [700], 2, 2, 128, 16),
+    ([1] * 65, [64 * (b % 5) + b for b in range(65)], 8, 2, 128, 16),       # just more sequences than lanes
+    ([(3 * b) % 7 for b in range(300)], [(3 * b) % 7 + (97 * b) % 150 for b in range(300)], 4, 4, 64, 16),
+    ([1] * 90 + [40], [5] * 89 + [6000, 300], 4, 4, 64, 32),               # one long context among many short ones
+    ([1] * 1100, [b % 23 for b in range(1100)], 1, 1, 64, 16),             # more sequences than a workgroup deals at once
+    ([1] * 1030 + [20], [3] * 1030 + [2000], 2, 1, 64, 16), ([256], [2300], 8, 8, 64, 128), ([65], [64 * 20 + 1], 6, 2, 128, 48), ([700], [700], 2, 2, 128, 16),
 ]
 
 
@@ -75,7 +79,7 @@ def test_attention_matches_the_definition(rf, case, causal):
     assert torch.equal(o.view(torch.int16), again.view(torch.int16))       # the same bits every time
 
 
-@pytest.mark.parametrize("case", (0, 3, 4, 5, 6, 7, 9, 11, 12, 14, 15, 16))
+@pytest.mark.parametrize("case", (0, 3, 4, 5, 6, 7, 9, 11, 12, 14, 15, 18, 21, 22))
 def test_attention_8_bit_cache(rf, case):
     n, k, Hq, Hkv, d, page = ATTENTION[case]
     say(f"paged attention, 8-bit cache {n[:6]} {k[:6]} Hq={Hq} Hkv={Hkv} d={d} page={page}")
