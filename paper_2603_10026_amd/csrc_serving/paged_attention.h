@@ -43,8 +43,13 @@ __device__ __forceinline__ void note_tile(const PagedArgs& a, int unit, bool fou
   }
 }
 
+// Workgroups of a launch, for the shares that there may be (of few rows: whole turns over the 8 XCDs).
+inline int64_t rows_blocks(const PagedArgs& a) { return ((int64_t)a.n_tiles + a.deal.target() + 7) / 8 * 8 * a.p.Hkv; }
+inline int64_t tiles_blocks(const PagedArgs& a) { return ((int64_t)a.n_tiles + a.deal.target()) * a.p.Hkv; }
+
 hipError_t launch_paged_rows(const PagedArgs& a, bool fp8, hipStream_t s);   // tiles of 16 or 32 rows
 hipError_t launch_paged_tiles(const PagedArgs& a, bool fp8, hipStream_t s);  // tiles of 128 rows
+hipError_t launch_paged_both(const PagedArgs& few, const PagedArgs& many, bool fp8, hipStream_t s);  // of 16, of 128
 constexpr int kTilesRowsLog2 = 7;
 
 }  // namespace rf

@@ -103,11 +103,12 @@ struct Plan {
 
 constexpr int kRoundsRows = 4, kRoundsTiles = 2;  // see chunk_keys_of()
 
-// Two workgroups to each of the 256 compute units.
-int round_of(const Paged& p, int64_t tiles, int rounds) {
+// Two workgroups to each of the 256 compute units; one, where the two kinds share the chip.
+int round_of(const Paged& p, int64_t tiles, bool alone) {
+  const int workgroups = alone ? 512 : 256;
   // no sequence is long enough, or there are so many workgroups that one long sequence more or less does not matter
-  if ((int64_t)p.table_len * p.page <= kLeastChunk || tiles * p.Hkv > 32 * 512 || p.Hkv > 512) return 0;
-  return 512 / p.Hkv;
+  if ((int64_t)p.table_len * p.page <= kLeastChunk || tiles * p.Hkv > 32 * 512 || p.Hkv > workgroups) return 0;
+  return workgroups / p.Hkv;
 }
 
 Plan plan_of(const Paged& p, int64_t max_q, bool cut) {
@@ -121,11 +122,11 @@ Plan plan_of(const Paged& p, int64_t max_q, bool cut) {
   const int few_log2 = few_only && rows > 16 ? 5 : 4;
   if (!many_only) {
     w.tiles[0] = few_only ? most_tiles(p, few_log2) : p.B < p.T ? p.B : p.T;
-    w.deal[0] = Deal{few_log2, 0, few_only ? INT32_MAX : 16, cut ? round_of(p, w.tiles[0], kRoundsRows) : 0, kRoundsRows};
+    w.deal[0] = Deal{few_log2, 0, few_only ? INT32_MAX : 16, cut ? round_of(p, w.tiles[0], few_only) : 0, kRoundsRows};
   }
   if (!few_only) {
     w.tiles[1] = most_tiles(p, kTilesRowsLog2);
-    w.deal[1] = Deal{kTilesRowsLog2, many_only ? 0 : 16, INT32_MAX, cut ? round_of(p, w.tiles[1], kRoundsTiles) : 0, kRoundsTiles};
+    w.deal[1] = Deal{kTilesRowsLog2, many_only ? 0 : 16, INT32_MAX, cut ? round_of(p, w.tiles[1], many_only) : 0, kRoundsTiles};
   }
   return w;
 }
@@ -145,9 +146,7 @@ int64_t part_bytes(const Plan& w, const Paged& p, int i) {
 // (a grid holds less than 2^32 threads)
 bool paged_attention_fits(const Paged& p, int64_t max_q) {
   const Plan w = plan_of(p, max_q, true);
-  for (int i = 0; i < 2; ++i)
-    if ((w.tiles[i] + w.deal[i].target()) * p.Hkv > UINT32_MAX / 256) return false;
-  return true;
+  return (w.tiles[0] + w.deal[0].target() + 8 + w.tiles[1] + w.deal[1].target()) * p.Hkv <= UINT32_MAX / 256;
 }
 
 size_t paged_attention_bytes(const Paged& p, int64_t max_q) {
@@ -188,9 +187,11 @@ hipError_t launch_paged_attention(const PagedAttention& x, void* workspace, hipS
       j.per_tile[i] = (int)((most + turn - 1) / turn);
       j.blocks[i] = (int)(w.tiles[i] * p.Hkv * j.per_tile[i]);
     }
-    const hipError_t e = i == 0 ? launch_paged_rows(a, x.fp8, s) : launch_paged_tiles(a, x.fp8, s);
-    if (e != hipSuccess) return e;
   }
+  const hipError_t e = w.tiles[1] == 0   ? launch_paged_rows(j.part[0], x.fp8, s)
+                       : w.tiles[0] == 0 ? launch_paged_tiles(j.part[1], x.fp8, s)
+                                         : launch_paged_both(j.part[0], j.part[1], x.fp8, s);
+  if (e != hipSuccess) return e;
   const int blocks = j.blocks[0] + j.blocks[1];
   if (blocks == 0) return hipSuccess;
   if (p.d == 128) hipLaunchKernelGGL((paged_join_kernel<128>), dim3(blocks), dim3(kJoinThreads), 0, s, j);

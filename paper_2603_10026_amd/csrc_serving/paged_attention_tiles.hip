@@ -1,6 +1,6 @@
 // Attention of many new tokens a sequence over a paged cache: a prompt's chunk.
 //
-// The same cascade as in paged_attention_rows.hip.  A workgroup owns 128 packed rows (new tokens times the query heads
+// The same cascade as in paged_rows.h.  A workgroup owns 128 packed rows (new tokens times the query heads
 // that share a KV head, token by token, so that a causal tile's rows see nearly the same keys) and walks the keys in
 // tiles of 64, or one chunk of them; a wavefront owns 32 of the rows as columns of its 32x32x16 products:
 //   S^T = K Q^T        A = K tile (LDS), B = Q^T (registers, loaded once)
@@ -19,7 +19,7 @@
 
 #include <type_traits>
 
-#include "paged_attention.h"
+#include "paged_rows.h"
 
 namespace rf {
 
@@ -38,8 +38,18 @@ __host__ __device__ constexpr __forceinline__ int fV(int row) {
   return (D == 128) ? (((row & 3) << 2) | ((row >> 2) & 3)) : ((((row >> 1) & 1) << 2) | ((row >> 2) & 3));
 }
 
+template <int D>
+constexpr int tiles_lds_bytes() { return 4 * kBK * D * 2; }  // K, K, V, V
+
+struct TilesScratch {
+  ShareScratch share;
+  int bad;
+  uint32_t noted[8];  // keys edge0 .. edge0 + 255: a tile's rows differ by less than 128 keys
+};
+
+// block: of the launch's share of the grid; lds: tiles_lds_bytes(), 1024-byte aligned.
 template <int D, bool FP8>
-__global__ __launch_bounds__(kNW* kWave, 2) void paged_tiles_kernel(const PagedArgs a, int n_units) {
+__device__ __forceinline__ void paged_tiles(const PagedArgs& a, unsigned block, unsigned char* lds, TilesScratch* scratch) {
   constexpr int ES = FP8 ? 1 : 2;
   constexpr int KS = D / 16;                       // contraction steps of S^T
   constexpr int DT = D / 32;                       // 32-row tiles of O^T
@@ -51,9 +61,6 @@ __global__ __launch_bounds__(kNW* kWave, 2) void paged_tiles_kernel(const PagedA
   constexpr int kRpl = kWave / kLpr;               // rows a load
   constexpr int kLd = kRows / kRpl;                // loads of K, and of V, a tile
   static_assert(kRows == 16, "one page for a wavefront's share of a tile");
-  __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * TILEB];  // K, K, V, V
-  __shared__ int s_bad;
-  __shared__ uint32_t s_noted[8];  // keys edge0 .. edge0 + 255: a tile's rows differ by less than 128 keys
 
   const Paged& p = a.p;
   const int lane = threadIdx.x & 63;
@@ -62,12 +69,10 @@ __global__ __launch_bounds__(kNW* kWave, 2) void paged_tiles_kernel(const PagedA
 
   // Heads vary fastest, so that with 8 KV heads each XCD's L2 holds one head's keys; late tiles, which see the most
   // keys under a causal mask, come first.
-  const int block = __builtin_amdgcn_readfirstlane(blockIdx.x / p.Hkv);
-  const int hk = __builtin_amdgcn_readfirstlane(blockIdx.x - block * p.Hkv);
-  const int unit = n_units - 1 - block;
+  const int unit = __builtin_amdgcn_readfirstlane(block / (unsigned)p.Hkv);
+  const int hk = __builtin_amdgcn_readfirstlane(block - unit * p.Hkv);
   Share w;
-  __shared__ ShareScratch s_share;
-  const bool found = find_share(p, a.deal, unit, &s_share, &w);
+  const bool found = find_share(p, a.deal, unit, &scratch->share, true, &w);
   if (hk == 0 && wave == 0) note_tile(a, unit, found, w);
   if (!found) return;
 
@@ -80,8 +85,8 @@ __global__ __launch_bounds__(kNW* kWave, 2) void paged_tiles_kernel(const PagedA
   const int wg_last = __builtin_amdgcn_readfirstlane(last_key(min(rows, r0 + 128) - 1));
   const int wg_min_last = __builtin_amdgcn_readfirstlane(last_key(r0));
   const int edge0 = max(0, wg_min_last + 1) & ~(kBK - 1);  // first key of the first tile that not every row sees whole
-  if (threadIdx.x < 8) s_noted[threadIdx.x] = 0;
-  if (threadIdx.x == 0) s_bad = 0;
+  if (threadIdx.x < 8) scratch->noted[threadIdx.x] = 0;
+  if (threadIdx.x == 0) scratch->bad = 0;
   const int wave_last = wave_r0 < rows ? __builtin_amdgcn_readfirstlane(last_key(min(rows, wave_r0 + 32) - 1)) : -1;
   const int wave_min_last = wave_r0 < rows ? __builtin_amdgcn_readfirstlane(last_key(wave_r0)) : -1;
   const int my_r = min(wave_r0 + i32, rows - 1);
@@ -397,7 +402,7 @@ __global__ __launch_bounds__(kNW* kWave, 2) void paged_tiles_kernel(const PagedA
         x[i] = key <= wg_last ? x[i] & ~f : 0u;
       }
       if (key > wg_last || (key > wg_min_last && odd != 0)) *at = x;
-      if (key > wg_min_last && key <= wg_last && odd != 0) atomicOr(&s_noted[(key - edge0) >> 5], 1u << ((key - edge0) & 31));
+      if (key > wg_min_last && key <= wg_last && odd != 0) atomicOr(&scratch->noted[(key - edge0) >> 5], 1u << ((key - edge0) & 31));
     }
   };
 
@@ -431,7 +436,7 @@ __global__ __launch_bounds__(kNW* kWave, 2) void paged_tiles_kernel(const PagedA
   }
 
   for (int i = 0; i < 8 && first < n_tiles; ++i) {
-    for (uint32_t noted = __builtin_amdgcn_readfirstlane(s_noted[i]); noted != 0; noted &= noted - 1) {
+    for (uint32_t noted = __builtin_amdgcn_readfirstlane(scratch->noted[i]); noted != 0; noted &= noted - 1) {
       const int key = edge0 + 32 * i + __builtin_ctz(noted), at = (unsigned)key / (unsigned)p.page;
       int id = p.pages[(int64_t)w.b * p.table_pitch + at];
       id = id < 0 || id >= p.n_pages ? 0 : id;
@@ -452,9 +457,9 @@ __global__ __launch_bounds__(kNW* kWave, 2) void paged_tiles_kernel(const PagedA
   asm volatile("" : "+v"(lane_));
   l += __shfl_xor(l, 32, 64);
   __syncthreads();  // every wavefront is done with the last tile
-  if (bad != 0) s_bad = 1;
+  if (bad != 0) scratch->bad = 1;
   __syncthreads();
-  if (s_bad != 0) l = NAN;  // a page that the cache does not have (a wavefront has looked up a quarter of them)
+  if (scratch->bad != 0) l = NAN;  // a page that the cache does not have (a wavefront has looked up a quarter of them)
   if (l != l) m_ref = 0.f;  // (a row of NaN may have no maximum, and is no empty state)
   if (w.chunks > 1) {
     constexpr int kPitch = D + 4, kQuads = D / 4, kHalf = 16;  // 16 rows at a time
@@ -515,22 +520,58 @@ __global__ __launch_bounds__(kNW* kWave, 2) void paged_tiles_kernel(const PagedA
   }
 }
 
+template <int D, bool FP8>
+__global__ __launch_bounds__(kNW* kWave, 2) void paged_tiles_kernel(const PagedArgs a) {
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[tiles_lds_bytes<D>()];
+  __shared__ TilesScratch scratch;
+  paged_tiles<D, FP8>(a, blockIdx.x, lds, &scratch);
+}
+
+// A batch of both kinds in one launch: sequences of few rows wait for memory while those of many keep the matrix unit
+// busy.  The tiles go first, since they last longest (us, in a launch each / this / taking turns eight workgroups at a
+// time; 1 sequence of 16 brings new tokens: 32 sequences of 512 over up to 4096 keys, d = 64, 56.5 / 46.1 / 54, 16 of
+// 2048 over 8000, d = 128, 314 / 294 / 375, 16 of 64 over 600 19.5 / 13.0 / 13.4).
+template <int D, bool FP8>
+__global__ __launch_bounds__(kNW* kWave, 2) void paged_both_kernel(const PagedArgs few, const PagedArgs many, unsigned many_blocks) {
+  static_assert(kWaves == kNW, "one size of workgroup");
+  constexpr int kLds = tiles_lds_bytes<D>() > rows_lds_bytes<D, 1, FP8>() ? tiles_lds_bytes<D>() : rows_lds_bytes<D, 1, FP8>();
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[kLds];
+  __shared__ TilesScratch scratch;
+  if (blockIdx.x < many_blocks) paged_tiles<D, FP8>(many, blockIdx.x, lds, &scratch);
+  else paged_rows<D, 1, FP8>(few, blockIdx.x - many_blocks, lds, &scratch.share);
+}
+
 }  // namespace
 
+#define RF_BY_TYPE(RF_LAUNCH)                  \
+  if (p.d == 128) {                            \
+    if (fp8) RF_LAUNCH(128, true);             \
+    else RF_LAUNCH(128, false);                \
+  } else {                                     \
+    if (fp8) RF_LAUNCH(64, true);              \
+    else RF_LAUNCH(64, false);                 \
+  }                                            \
+  return hipGetLastError()
+
 hipError_t launch_paged_tiles(const PagedArgs& a, bool fp8, hipStream_t s) {
-  const int64_t units = (int64_t)a.n_tiles + a.deal.target(), grid = units * a.p.Hkv;
+  const Paged& p = a.p;
+  const int64_t grid = tiles_blocks(a);
   if (grid > UINT32_MAX / (kNW * kWave)) return hipErrorInvalidValue;
-#define RF_TILES(DD, F8) \
-  hipLaunchKernelGGL((paged_tiles_kernel<DD, F8>), dim3((unsigned)grid), dim3(kNW * kWave), 0, s, a, (int)units)
-  if (a.p.d == 128) {
-    if (fp8) RF_TILES(128, true);
-    else RF_TILES(128, false);
-  } else {
-    if (fp8) RF_TILES(64, true);
-    else RF_TILES(64, false);
-  }
+#define RF_TILES(DD, F8) hipLaunchKernelGGL((paged_tiles_kernel<DD, F8>), dim3((unsigned)grid), dim3(kNW * kWave), 0, s, a)
+  RF_BY_TYPE(RF_TILES);
 #undef RF_TILES
-  return hipGetLastError();
 }
+
+hipError_t launch_paged_both(const PagedArgs& few, const PagedArgs& many, bool fp8, hipStream_t s) {
+  const Paged& p = few.p;
+  const int64_t nf = rows_blocks(few), nm = tiles_blocks(many);
+  if (nf + nm > UINT32_MAX / (kNW * kWave)) return hipErrorInvalidValue;
+#define RF_BOTH(DD, F8)                                                                                          \
+  hipLaunchKernelGGL((paged_both_kernel<DD, F8>), dim3((unsigned)(nf + nm)), dim3(kNW * kWave), 0, s, few, many, \
+                     (unsigned)nm)
+  RF_BY_TYPE(RF_BOTH);
+#undef RF_BOTH
+}
+#undef RF_BY_TYPE
 
 }  // namespace rf

@@ -121,8 +121,10 @@ struct ShareScratch {
 // Share number `unit` of the batch; false past the last one.  Shares are counted sequence by sequence, tile by tile.
 // There are at most target + tiles of them, and at most 2 target with more than one chunk to their tile: such a tile has
 // over chunk_keys keys, so ceil(keys / chunk_keys) is below twice keys / chunk_keys, and the sum of all keys / chunk_keys
-// is at most target.  Called by whole workgroups of 256 threads.
-__device__ __forceinline__ bool find_share(const Paged& p, const Deal& d, int unit, ShareScratch* scratch, Share* out) {
+// is at most target.  Called by whole workgroups of 256 threads.  last_first: shares of batches of up to 64 sequences
+// are numbered from the last one on.
+__device__ __forceinline__ bool find_share(const Paged& p, const Deal& d, int unit, ShareScratch* scratch, bool last_first,
+                                           Share* out) {
   const int lane = threadIdx.x & 63;
   auto units_of = [](const Sequence& x) { return (unsigned)(x.len + 63) >> 6; };
   if (p.B <= kWave) {
@@ -140,9 +142,11 @@ __device__ __forceinline__ bool find_share(const Paged& p, const Deal& d, int un
     }
     const int chunks = chunks_of(s.len, chunk_keys);
     const int upto = wave_inclusive_scan(tiles * chunks), slots_upto = wave_inclusive_scan(chunks > 1 ? tiles * chunks : 0);
+    const int all_shares = __builtin_amdgcn_readlane(upto, 63);
+    if (last_first && unit < all_shares) unit = all_shares - 1 - unit;
     const uint64_t past = __builtin_amdgcn_ballot_w64(upto > unit);
     if (past == 0) {
-      out->all_shares = __builtin_amdgcn_readlane(upto, 63);
+      out->all_shares = all_shares;
       out->all_tiles = all_tiles;
       return false;
     }
