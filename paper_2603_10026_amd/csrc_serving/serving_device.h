@@ -67,6 +67,7 @@ struct Deal {
   int rows_log2, lo_rows, hi_rows;
   int round;   // shares that the chip takes at once, for one KV head; 0: nothing is cut
   int rounds;  // of the chunks of long contexts
+  int slack;   // eighths of a workgroup's share of one round that the longest tile may have more
   __host__ __device__ int target() const { return round * rounds; }
 };
 constexpr int kLeastChunk = 128;   // keys
@@ -82,7 +83,11 @@ struct Share {
 
 // Keys of a chunk, a multiple of 128, or INT32_MAX: from the tiles of the batch, the keys that they have together and
 // the longest one's, these in units of 64 (so that 32 bits hold the sum).
-//  - A batch whose longest tile is little more than a workgroup's share of one round is not cut.
+//  - A batch whose longest tile is little more than a workgroup's share of one round is not cut.  (slack: little is an
+//    eighth where a chunk's state is small.  A tile of 128 rows leaves 66 KB for a chunk, which the joining launch reads
+//    again: 7 eighths.  us at 1 / 4 / 8 eighths, 32 heads over 8, d = 128: 8 sequences of 300 new tokens over 600 to 3000
+//    keys 165 / 141 / 137, 2 of 1024 over 800 to 8000 259 / 214 / 213; one of 1024 over 16000, 2 tiles a share,
+//    296 / 302 / 316.)
 //  - Little work goes in one round: a second one would cost a workgroup's way into the cache (the arrays, the page
 //    table, the first keys: three trips to memory) again.  Every sequence's last chunk is half empty on average.
 //  - Much goes in several, so that unequal last chunks do not leave the chip idle at the end.
@@ -91,7 +96,7 @@ struct Share {
 __device__ __forceinline__ int chunk_keys_of(const Deal& d, unsigned tiles, unsigned units, unsigned longest) {
   if (d.round == 0) return INT32_MAX;
   const unsigned even = (units + d.round - 1) / (unsigned)d.round;
-  if (longest <= even + even / 8) return INT32_MAX;
+  if (longest <= even + even * d.slack / 8) return INT32_MAX;
   unsigned share;
   if (even <= kLongShare) {
     const unsigned left = tiles < (unsigned)d.round ? d.round - tiles / 2 : d.round;
