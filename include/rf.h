@@ -329,7 +329,10 @@ RF_API rf_status rf_paged_append(const rf_tensor* q, const rf_tensor* k, const r
  *   q, o : [T, Hq, d] bf16, Hq % Hkv == 0.
  *   causal != 0: token i of n sees keys j <= kv_len - n + i, otherwise all keys.  A row that sees none produces zeros,
  *       and what an unseen slot holds (NaN too) does not show.
+ *   o must not overlap the inputs.
  *   max_q : tokens of the longest sequence, for the choice of kernels; results are right for any value >= 0.
+ *   Rounding: probabilities to bf16 before the second product, o to bf16 at the end, everything between in fp32.  The
+ *   kernel and the cuts of the keys follow from the whole batch: a row's last bits may differ from one batch to another.
  * Rows that see a key whose page is not in the cache are NaN (others of the same sequence may be), and so are all rows
  * of a sequence with more keys than the table has room for.
  */

@@ -45,7 +45,7 @@ rf_status paged_shape(const rf_tensor* q, const rf_tensor* cache, const rf_tenso
   if ((st = check_tensor(pages, 2, 2, RF_I32)) != RF_OK) return st;
   if (q->dtype != RF_BF16 || cache->dtype == RF_F32 || pages->dtype != RF_I32) return RF_ERR_UNSUPPORTED;
   const int64_t T = q->shape[0], Hq = q->shape[1], d = q->shape[2], page = cache->shape[1], Hkv = cache->shape[2];
-  if (cache->shape[3] != d || Hkv < 1 || Hq % Hkv != 0) return RF_ERR_INVALID_ARG;
+  if (cache->shape[3] != d || Hkv < 1 || Hq < 1 || Hq % Hkv != 0) return RF_ERR_INVALID_ARG;
   if ((d != 64 && d != 128) || page < 16 || page % 16 != 0) return RF_ERR_UNSUPPORTED;
   if (!rows_contiguous(cache) || !rows_contiguous(pages)) return RF_ERR_UNSUPPORTED;
   if (cache->stride[1] > ((int64_t)1 << 26)) return RF_ERR_UNSUPPORTED;  // 32-bit offsets inside 16 slots

@@ -104,11 +104,14 @@ struct Plan {
 constexpr int kRoundsRows = 4, kRoundsTiles = 2, kSlackRows = 1, kSlackTiles = 7;  // see chunk_keys_of()
 
 // Two workgroups to each of the 256 compute units; one, where the two kinds share the chip.
-int round_of(const Paged& p, int64_t tiles, bool alone) {
+int round_of(const Paged& p, int64_t tiles, bool alone, int rows_log2, int slack) {
   const int workgroups = alone ? 512 : 256;
   // no sequence is long enough, or there are so many workgroups that one long sequence more or less does not matter
   if ((int64_t)p.table_len * p.page <= kLeastChunk || tiles * p.Hkv > 32 * 512 || p.Hkv > workgroups) return 0;
-  return workgroups / p.Hkv;
+  const int round = workgroups / p.Hkv;
+  // one sequence of so many tiles that none is over its share: whatever its length, nothing to join
+  if (p.B == 1 && ((((int64_t)p.T * p.group - 1) >> rows_log2) + 1) * (8 + slack) >= 8 * (int64_t)round) return 0;
+  return round;
 }
 
 Plan plan_of(const Paged& p, int64_t max_q, bool cut) {
@@ -122,11 +125,11 @@ Plan plan_of(const Paged& p, int64_t max_q, bool cut) {
   const int few_log2 = few_only && rows > 16 ? 5 : 4;
   if (!many_only) {
     w.tiles[0] = few_only ? most_tiles(p, few_log2) : p.B < p.T ? p.B : p.T;
-    w.deal[0] = Deal{few_log2, 0, few_only ? INT32_MAX : 16, cut ? round_of(p, w.tiles[0], few_only) : 0, kRoundsRows, kSlackRows};
+    w.deal[0] = Deal{few_log2, 0, few_only ? INT32_MAX : 16, cut ? round_of(p, w.tiles[0], few_only, few_log2, kSlackRows) : 0, kRoundsRows, kSlackRows};
   }
   if (!few_only) {
     w.tiles[1] = most_tiles(p, kTilesRowsLog2);
-    w.deal[1] = Deal{kTilesRowsLog2, many_only ? 0 : 16, INT32_MAX, cut ? round_of(p, w.tiles[1], many_only) : 0, kRoundsTiles, kSlackTiles};
+    w.deal[1] = Deal{kTilesRowsLog2, many_only ? 0 : 16, INT32_MAX, cut ? round_of(p, w.tiles[1], many_only, kTilesRowsLog2, kSlackTiles) : 0, kRoundsTiles, kSlackTiles};
   }
   return w;
 }

@@ -71,7 +71,7 @@ struct Deal {
   __host__ __device__ int target() const { return round * rounds; }
 };
 constexpr int kLeastChunk = 128;   // keys
-constexpr int kLongShare = 32;     // of 64 keys each: a workgroup's in one round, from which on a context is long
+constexpr int kLongShare = 2048;   // keys: a workgroup's in one round, from which on contexts are long
 
 struct Share {
   Sequence s;
@@ -81,8 +81,15 @@ struct Share {
   int all_shares, all_tiles;  // of the batch (where there is no such share)
 };
 
+// The unit that find_share() counts keys in, as a power of 2: 64 for tables of up to 2^23 keys a sequence, and so much
+// larger for longer ones that 32 bits hold the sum over a launch that may cut (at most 2^14 tiles).
+__device__ __forceinline__ int unit_log2_of(const Paged& p) {
+  const int most = capacity_of(p);
+  return most <= 1 << 23 ? 6 : 32 - __clz(most - 1) - 17;
+}
+
 // Keys of a chunk, a multiple of 128, or INT32_MAX: from the tiles of the batch, the keys that they have together and
-// the longest one's, these in units of 64 (so that 32 bits hold the sum).
+// the longest one's, these in units.
 //  - A batch whose longest tile is little more than a workgroup's share of one round is not cut.  (slack: little is an
 //    eighth where a chunk's state is small.  A tile of 128 rows leaves 66 KB for a chunk, which the joining launch reads
 //    again: 7 eighths.  us at 1 / 4 / 8 eighths, 32 heads over 8, d = 128: 8 sequences of 300 new tokens over 600 to 3000
@@ -93,18 +100,18 @@ struct Share {
 //  - Much goes in several, so that unequal last chunks do not leave the chip idle at the end.
 // us of a decode step, 32 heads over 8, d = 128, with chunks for one round / two / four: 64 contexts of 400 to 8192
 // 229 / 210 / 203; one of 32768 34 / 40 / 43; 8 of 2000 19 / 20 / 21.
-__device__ __forceinline__ int chunk_keys_of(const Deal& d, unsigned tiles, unsigned units, unsigned longest) {
+__device__ __forceinline__ int chunk_keys_of(const Deal& d, unsigned tiles, unsigned units, unsigned longest, int unit_log2) {
   if (d.round == 0) return INT32_MAX;
   const unsigned even = (units + d.round - 1) / (unsigned)d.round;
   if (longest <= even + even * d.slack / 8) return INT32_MAX;
   unsigned share;
-  if (even <= kLongShare) {
+  if (even <= (unsigned)(kLongShare >> unit_log2)) {
     const unsigned left = tiles < (unsigned)d.round ? d.round - tiles / 2 : d.round;
     share = (units + left - 1) / left;
   } else {
     share = (units + d.target() - 1) / (unsigned)d.target();
   }
-  return (int)min(((uint64_t)share * 64 + 127) & ~(uint64_t)127, (uint64_t)(INT32_MAX - 127));
+  return (int)min((((uint64_t)share << unit_log2) + 127) & ~(uint64_t)127, (uint64_t)(INT32_MAX - 127));
 }
 
 __device__ __forceinline__ unsigned chunks_of(int len, int chunk_keys) {
@@ -131,7 +138,8 @@ struct ShareScratch {
 __device__ __forceinline__ bool find_share(const Paged& p, const Deal& d, int unit, ShareScratch* scratch, bool last_first,
                                            Share* out) {
   const int lane = threadIdx.x & 63;
-  auto units_of = [](const Sequence& x) { return (unsigned)(x.len + 63) >> 6; };
+  const int unit_log2 = unit_log2_of(p);
+  auto units_of = [&](const Sequence& x) { return ((unsigned)x.len + (1u << unit_log2) - 1) >> unit_log2; };
   if (p.B <= kWave) {
     // a sequence to a lane, in every wavefront
     Sequence s{0, 0, 0, false};
@@ -141,9 +149,8 @@ __device__ __forceinline__ bool find_share(const Paged& p, const Deal& d, int un
     int chunk_keys = INT32_MAX;
     if (d.round > 0) {
       const unsigned units = __builtin_amdgcn_readlane(wave_inclusive_scan(tiles * units_of(s)), 63);
-      // (exact below 2^24; sequences beyond are cut anyway)
       const unsigned longest = (unsigned)wave_max(tiles > 0 ? (float)units_of(s) : 0.f);
-      chunk_keys = __builtin_amdgcn_readfirstlane(chunk_keys_of(d, all_tiles, units, longest));
+      chunk_keys = __builtin_amdgcn_readfirstlane(chunk_keys_of(d, all_tiles, units, longest, unit_log2));
     }
     const int chunks = chunks_of(s.len, chunk_keys);
     const int upto = wave_inclusive_scan(tiles * chunks), slots_upto = wave_inclusive_scan(chunks > 1 ? tiles * chunks : 0);
@@ -209,7 +216,7 @@ __device__ __forceinline__ bool find_share(const Paged& p, const Deal& d, int un
     __syncthreads();
     auto sum = [&](int k) { return (unsigned)(scratch->totals[k][0] + scratch->totals[k][1] + scratch->totals[k][2] + scratch->totals[k][3]); };
     longest = max(max(scratch->totals[2][0], scratch->totals[2][1]), max(scratch->totals[2][2], scratch->totals[2][3]));
-    chunk_keys = __builtin_amdgcn_readfirstlane(chunk_keys_of(d, sum(1), sum(0), longest));
+    chunk_keys = __builtin_amdgcn_readfirstlane(chunk_keys_of(d, sum(1), sum(0), longest, unit_log2));
     if (p.B > kBlock) load(0);
   }
   int base = 0, slot_base = 0, tile_base = 0;

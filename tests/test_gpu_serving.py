@@ -165,6 +165,18 @@ def test_attention_arrays_of_nonsense_stay_inside(rf):
             assert bool(torch.isnan(o.float()[:12]).all())
 
 
+def test_attention_tables_with_room_for_millions_of_keys(rf):
+    """Long rows of the page table (keys are then counted in larger units), sequences of ordinary lengths."""
+    say("paged attention, a table of 2^24 keys")
+    for n, k in (([1, 1, 5], [3000, 40, 700]), ([1, 130], [900, 1500])):
+        bt = sb.Batch(370, n, k, 8, 2, 64, 16)
+        want = expect(bt)
+        wide = np.full((len(n), (1 << 24) // 16), -5, np.int32)
+        wide[:, :bt.table.shape[1]] = bt.table
+        bt.table = wide
+        sb.check_attention(attend(rf, bt), *want, max(k), "wide table")
+
+
 def test_attention_offsets_past_32_bits(rf):
     """A cache of over 2^32 elements (9 GB each), its pages at both ends."""
     say("paged attention and append, offsets past 32 bits")
@@ -201,6 +213,8 @@ APPEND = [
     ([3, 4], [1, 9], 5, 1, 128, 16, 96, False, False),                     # tokens without a position
     ([9], [20], 1, 1, 64, 16, 16, False, True), ([9], [20], 3, 1, 64, 16, 48, True, False), ([5], [77], 7, 7, 128, 80, 0, False, True),
     ([5, 1], [77, 12], 7, 7, 64, 16, 0, False, False),
+    ([3, 2], [30, 40], 4, 2, 64, 16, 64, False, "q"), ([3, 2], [30, 40], 4, 2, 128, 16, 64, True, "k"),   # one norm alone
+    ([600], [600], 16, 2, 64, 16, 64, False, True), ([700], [701], 8, 8, 128, 64, 128, False, True),       # many tokens
 ]
 
 
@@ -211,7 +225,7 @@ def tables(rot, rows):
 
 def run_append(rf, bt, rot, interleaved, norms, rows=None, in_place=False, strided=False):
     r = np.random.default_rng(5)
-    g = [sb.bf16(1 + 0.3 * r.standard_normal(bt.d)) if norms else None for _ in range(2)]
+    g = [sb.bf16(1 + 0.3 * r.standard_normal(bt.d)) if norms and norms != skip else None for skip in ("k", "q")]
     cs = tables(rot, rows or max(bt.k) + 3) if rot else (None, None)
     k, v = (sb.cache_on(c, DEV) for c in bt.caches)
     if strided:

@@ -44,7 +44,7 @@ PAGED = [
     (dict(vc=_desc([10, 16, 2, 128], F8)), UNS), (dict(vc=_desc([10, 32, 2, 128])), BAD),
     (dict(vc=_desc([10, 16, 2, 128], stride=[8192, 256, 128, 1])), UNS),                     # other strides than the keys'
     (dict(kc=_desc([10, 16, 3, 128]), vc=_desc([10, 16, 3, 128])), BAD),                     # 8 heads over 3
-    (dict(d=96), UNS), (dict(page=8), UNS), (dict(page=24), UNS),
+    (dict(q=_desc([7, 0, 128]), out=_desc([7, 0, 128])), BAD), (dict(d=96), UNS), (dict(page=8), UNS), (dict(page=24), UNS),
     (dict(starts=_desc([3], I32)), BAD), (dict(lens=_desc([4], I32)), BAD), (dict(starts=_desc([4], F32)), UNS),
     (dict(lens=_desc([3], I32, stride=[2])), UNS), (dict(pages=_desc([3, 4], F32)), UNS),
     (dict(pages=_desc([3, 4], I32, stride=[8, 2])), UNS), (dict(ks=0.5), BAD), (dict(vs=float("nan")), BAD),
