@@ -125,11 +125,13 @@ Plan plan_of(const Paged& p, int64_t max_q, bool cut) {
   const int few_log2 = few_only && rows > 16 ? 5 : 4;
   if (!many_only) {
     w.tiles[0] = few_only ? most_tiles(p, few_log2) : p.B < p.T ? p.B : p.T;
-    w.deal[0] = Deal{few_log2, 0, few_only ? INT32_MAX : 16, cut ? round_of(p, w.tiles[0], few_only, few_log2, kSlackRows) : 0, kRoundsRows, kSlackRows};
+    w.deal[0] = Deal{few_log2, 0, few_only ? INT32_MAX : 16, cut ? round_of(p, w.tiles[0], few_only, few_log2, kSlackRows) : 0,
+                     kRoundsRows, kSlackRows};
   }
   if (!few_only) {
     w.tiles[1] = most_tiles(p, kTilesRowsLog2);
-    w.deal[1] = Deal{kTilesRowsLog2, many_only ? 0 : 16, INT32_MAX, cut ? round_of(p, w.tiles[1], many_only, kTilesRowsLog2, kSlackTiles) : 0, kRoundsTiles, kSlackTiles};
+    w.deal[1] = Deal{kTilesRowsLog2, many_only ? 0 : 16, INT32_MAX,
+                     cut ? round_of(p, w.tiles[1], many_only, kTilesRowsLog2, kSlackTiles) : 0, kRoundsTiles, kSlackTiles};
   }
   return w;
 }

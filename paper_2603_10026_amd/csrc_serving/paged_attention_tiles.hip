@@ -72,7 +72,7 @@ __device__ __forceinline__ void paged_tiles(const PagedArgs& a, unsigned block, 
   const int unit = __builtin_amdgcn_readfirstlane(block / (unsigned)p.Hkv);
   const int hk = __builtin_amdgcn_readfirstlane(block - unit * p.Hkv);
   Share w;
-  const bool found = find_share(p, a.deal, unit, &scratch->share, true, &w);
+  const bool found = find_share(p, a.deal, a.n_tiles, unit, &scratch->share, true, &w);
   if (hk == 0 && wave == 0) note_tile(a, unit, found, w);
   if (!found) return;
 

@@ -58,8 +58,6 @@ __device__ __forceinline__ void paged_rows(const PagedArgs& a, unsigned block, u
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int i16 = lane & 15, g = lane >> 4;
 
-  // Workgroups are dealt round-robin to the 8 XCDs: the KV heads of a share go to one of them, one behind the other.
-  // Their rows lie side by side in memory, and the XCD's address translation and page table lookups serve all of them.
   // Workgroups are dealt round-robin to the 8 XCDs.  Rows of up to 128 bytes: the KV heads of a share go to one of them,
   // one behind the other, so that its address translation serves neighbouring heads' rows together (32 contexts of 32768
   // in FP8, d = 128, 425 -> 402 us); longer rows gain nothing by it (64 contexts of 4300 in bf16 207 -> 213).
@@ -73,7 +71,7 @@ __device__ __forceinline__ void paged_rows(const PagedArgs& a, unsigned block, u
     hk = __builtin_amdgcn_readfirstlane(block - unit * p.Hkv);
   }
   Share w;
-  const bool found = find_share(p, a.deal, unit, scratch, false, &w);
+  const bool found = find_share(p, a.deal, a.n_tiles, unit, scratch, false, &w);
   if (hk == 0 && wave == 0) note_tile(a, unit, found, w);
   if (!found) return;
 

@@ -133,10 +133,11 @@ struct ShareScratch {
 // Share number `unit` of the batch; false past the last one.  Shares are counted sequence by sequence, tile by tile.
 // There are at most target + tiles of them, and at most 2 target with more than one chunk to their tile: such a tile has
 // over chunk_keys keys, so ceil(keys / chunk_keys) is below twice keys / chunk_keys, and the sum of all keys / chunk_keys
-// is at most target.  Called by whole workgroups of 256 threads.  last_first: shares of batches of up to 64 sequences
+// is at most target.  All of this holds for sequences that do not overlap; where the arrays say nonsense and more tiles
+// come of it than the host has counted (n_tiles), the batch has no shares.  Called by whole workgroups of 256 threads.  last_first: shares of batches of up to 64 sequences
 // are numbered from the last one on.
-__device__ __forceinline__ bool find_share(const Paged& p, const Deal& d, int unit, ShareScratch* scratch, bool last_first,
-                                           Share* out) {
+__device__ __forceinline__ bool find_share(const Paged& p, const Deal& d, int n_tiles, int unit, ShareScratch* scratch,
+                                           bool last_first, Share* out) {
   const int lane = threadIdx.x & 63;
   const int unit_log2 = unit_log2_of(p);
   auto units_of = [&](const Sequence& x) { return ((unsigned)x.len + (1u << unit_log2) - 1) >> unit_log2; };
@@ -145,7 +146,12 @@ __device__ __forceinline__ bool find_share(const Paged& p, const Deal& d, int un
     Sequence s{0, 0, 0, false};
     if (lane < p.B) s = load_sequence(p, lane);
     const int tiles = tiles_of(p, d, s);
+    // (no sequence has more tiles than n_tiles, which a grid's size keeps below 2^24: the sum does not wrap)
     const int tiles_upto = wave_inclusive_scan(tiles), all_tiles = __builtin_amdgcn_readlane(tiles_upto, 63);
+    if (all_tiles > n_tiles) {
+      out->all_shares = out->all_tiles = 0;
+      return false;
+    }
     int chunk_keys = INT32_MAX;
     if (d.round > 0) {
       const unsigned units = __builtin_amdgcn_readlane(wave_inclusive_scan(tiles * units_of(s)), 63);
@@ -190,35 +196,43 @@ __device__ __forceinline__ bool find_share(const Paged& p, const Deal& d, int un
     }
   };
   load(0);
-  int chunk_keys = INT32_MAX;
   if (threadIdx.x == 0) scratch->found = 0;
-  if (d.round > 0) {
-    unsigned units = 0, longest = 0, all = 0;
-    for (int b0 = 0;;) {
+  unsigned units = 0, longest = 0;
+  float all = 0.f;
+  for (int b0 = 0;;) {
 #pragma unroll
-      for (int i = 0; i < kEach; ++i) {
-        units += tiles[i] * units_of(s[i]);
-        longest = max(longest, tiles[i] > 0 ? units_of(s[i]) : 0);
-        all += tiles[i];
-      }
-      b0 += kBlock;
-      if (b0 >= p.B) break;
-      load(b0);
+    for (int i = 0; i < kEach; ++i) {
+      units += tiles[i] * units_of(s[i]);
+      longest = max(longest, tiles[i] > 0 ? units_of(s[i]) : 0);
+      all += (float)tiles[i];
     }
-    units = wave_inclusive_scan(units);
-    all = wave_inclusive_scan(all);
-    longest = (unsigned)wave_max((float)longest);
-    if (lane == 63) {
-      scratch->totals[0][wave] = units;
-      scratch->totals[1][wave] = all;
-      scratch->totals[2][wave] = longest;
-    }
-    __syncthreads();
-    auto sum = [&](int k) { return (unsigned)(scratch->totals[k][0] + scratch->totals[k][1] + scratch->totals[k][2] + scratch->totals[k][3]); };
-    longest = max(max(scratch->totals[2][0], scratch->totals[2][1]), max(scratch->totals[2][2], scratch->totals[2][3]));
-    chunk_keys = __builtin_amdgcn_readfirstlane(chunk_keys_of(d, sum(1), sum(0), longest, unit_log2));
-    if (p.B > kBlock) load(0);
+    b0 += kBlock;
+    if (b0 >= p.B) break;
+    load(b0);
   }
+  units = wave_inclusive_scan(units);
+  all = wave_sum(all);
+  longest = (unsigned)wave_max((float)longest);
+  if (lane == 63) {
+    scratch->totals[0][wave] = units;
+    scratch->totals[1][wave] = (int)fminf(all, 1e9f);
+    scratch->totals[2][wave] = longest;
+  }
+  __syncthreads();
+  units = longest = 0;
+  all = 0.f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    units += scratch->totals[0][i];
+    all += (float)scratch->totals[1][i];
+    longest = max(longest, (unsigned)scratch->totals[2][i]);
+  }
+  if (__builtin_amdgcn_readfirstlane(all > (float)n_tiles)) {
+    out->all_shares = out->all_tiles = 0;
+    return false;
+  }
+  const int chunk_keys = __builtin_amdgcn_readfirstlane(chunk_keys_of(d, (unsigned)all, units, longest, unit_log2));
+  if (p.B > kBlock) load(0);
   int base = 0, slot_base = 0, tile_base = 0;
   for (int b0 = 0;;) {
     int mine = 0, slots = 0, here = 0, chunks[kEach];

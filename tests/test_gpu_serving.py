@@ -154,15 +154,33 @@ def test_attention_bad_pages_and_overlong_sequences_are_nan(rf):
     assert bool((attend(rf, bt) == 0).all())
 
 
-def test_attention_arrays_of_nonsense_stay_inside(rf):
-    """seq_start that descends or leaves the tokens: whatever comes out, rows of no sequence are left alone."""
-    say("paged attention and append, seq_start out of range")
-    bt = sb.Batch(350, [3, 3, 3], [30, 40, 50], 4, 2, 64, 16, tail=4)
-    for starts in ([5, 2, 40, 90], [-7, 3, 3, 6], [12, 12, 12, 12], [2 ** 31 - 1, -(2 ** 31), 0, 7]):
-        bt.seq_start = np.array(starts, np.int32)
-        o = attend(rf, bt)
-        if starts[0] == 12:
-            assert bool(torch.isnan(o.float()[:12]).all())
+@pytest.mark.parametrize("sequences", (3, 9, 200, 1200))
+def test_attention_arrays_of_nonsense_stay_inside(rf, sequences):
+    """seq_start that descends, leaves the tokens or names them many times over: whatever comes out, rows of no sequence
+    are left alone, and so is everything outside."""
+    say(f"paged attention and append, seq_start out of range, {sequences} sequences")
+    r = np.random.default_rng(351)
+    n = [3] * sequences
+    bt = sb.Batch(350, n, [400 if b < 3 else 7 for b in range(sequences)], 4, 2, 64, 16, tail=4)
+    T, B = bt.T, sequences
+    kinds = [np.full(B + 1, T - 1), np.where(np.arange(B + 1) % 2, T, 0), np.arange(B + 1)[::-1], r.integers(-T, 2 * T, B + 1),
+             r.integers(-(2 ** 31), 2 ** 31, B + 1), np.full(B + 1, 2 ** 31 - 1), np.full(B + 1, -(2 ** 31))]
+    guard = torch.full((T + 64, 4, 64), float("nan"), dtype=BF, device=DEV)
+    for i, starts in enumerate(kinds):
+        bt.seq_start = starts.astype(np.int32)
+        for max_q in (1, T):
+            say(f"  kind {i}, max_q {max_q}")
+            guard.fill_(float("nan"))
+            attend(rf, bt, max_q=max_q, o=guard[32:32 + T])
+            assert bool(torch.isnan(guard[:32].float()).all()) and bool(torch.isnan(guard[32 + T:].float()).all())
+            if i in (0, 5, 6):
+                assert bool(torch.isnan(guard[32:32 + T - 1].float()).all())
+        q, nk, nv = (x.to(DEV) for x in (bt.q, bt.new_k, bt.new_v))
+        k, v = (sb.cache_on(c, DEV) for c in bt.caches)
+        cos, sin = (torch.from_numpy(x).to(DEV) for x in tables(64, 500))
+        rf.rf_paged_append(q, nk, nv, k, v, *bt.on(DEV), cos=cos, sin=sin, q_out=guard[32:32 + T])
+        torch.cuda.synchronize()
+        assert bool(torch.isnan(guard[:32].float()).all()) and bool(torch.isnan(guard[32 + T:].float()).all())
 
 
 def test_attention_tables_with_room_for_millions_of_keys(rf):
