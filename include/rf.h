@@ -298,8 +298,9 @@ RF_API rf_status rf_rmsnorm_gemm_ws(const rf_tensor* x, const rf_tensor* g, cons
  *       kv_len[b] - n + i.  Where that is negative the token has neither (a captured batch's unused places: kv_len 0).
  *   seq_start: [B + 1] i32.
  * The three arrays are read on the device only, so a captured graph serves every batch that fits.  Whatever they say,
- * no access leaves the tensors.  A page number outside the cache, or more keys than max_pages has room for, is
- * answered by NaN (see the entry points).  T * Hq < 2^31.
+ * no access leaves the tensors (rows of sequences that overlap or run backwards may be left as they were).  A page
+ * number outside the cache, or more keys than max_pages has room for, is answered by NaN (see the entry points).
+ * T * Hq < 2^31.
  */
 
 /*

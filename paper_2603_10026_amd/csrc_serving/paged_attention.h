@@ -22,7 +22,8 @@ struct PagedArgs {
   bf16_t* o;
   Strides2 sq, so;
   float scale_log2e, v_scale;
-  int causal, n_tiles;  // n_tiles: entries of `tiles`
+  int causal;
+  int n_tiles, n_units;  // entries of `tiles`; shares that there may be
   float *part_acc, *part_m, *part_l;  // the maximum in log2 units; the sums not normalised
   JoinTile* tiles;
 };
@@ -37,15 +38,15 @@ __device__ __forceinline__ void note_tile(const PagedArgs& a, int unit, bool fou
       a.tiles[w.tile_index] = JoinTile{w.chunks, w.slot, w.s.row0 * a.p.group + r0, min(R, w.s.n * a.p.group - r0)};
   } else {
     // (units past the last share are at least as many as tiles past the last tile: a launch has n_tiles + target units,
-    // and shares are at most `target` more than tiles)
+    // and shares are at most `target` more than tiles; or n_tiles times the most chunks that a tile can have)
     const int64_t at = (int64_t)unit - w.all_shares + w.all_tiles;
     if (at < a.n_tiles) a.tiles[at] = JoinTile{1, 0, 0, 0};
   }
 }
 
 // Workgroups of a launch, for the shares that there may be (of few rows: whole turns over the 8 XCDs).
-inline int64_t rows_blocks(const PagedArgs& a) { return ((int64_t)a.n_tiles + a.deal.target() + 7) / 8 * 8 * a.p.Hkv; }
-inline int64_t tiles_blocks(const PagedArgs& a) { return ((int64_t)a.n_tiles + a.deal.target()) * a.p.Hkv; }
+inline int64_t rows_blocks(const PagedArgs& a) { return ((int64_t)a.n_units + 7) / 8 * 8 * a.p.Hkv; }
+inline int64_t tiles_blocks(const PagedArgs& a) { return (int64_t)a.n_units * a.p.Hkv; }
 
 hipError_t launch_paged_rows(const PagedArgs& a, bool fp8, hipStream_t s);   // tiles of 16 or 32 rows
 hipError_t launch_paged_tiles(const PagedArgs& a, bool fp8, hipStream_t s);  // tiles of 128 rows

@@ -136,10 +136,18 @@ Plan plan_of(const Paged& p, int64_t max_q, bool cut) {
   return w;
 }
 
-// Rows of the workspace: see find_share() for the number of chunks of tiles that have several.
+// Chunks of all tiles, if each had as many as the page table has room for.
+int64_t most_chunks(const Plan& w, const Paged& p, int i) {
+  return w.tiles[i] * (((int64_t)p.table_len * p.page + kLeastChunk - 1) / kLeastChunk);
+}
+// Shares that there may be, and rows of the workspace: see find_share().
+int64_t units_of(const Plan& w, const Paged& p, int i) {
+  if (w.deal[i].round == 0) return w.tiles[i];
+  const int64_t shares = w.tiles[i] + w.deal[i].target(), most = most_chunks(w, p, i);
+  return shares < most ? shares : most;
+}
 int64_t slots_of(const Plan& w, const Paged& p, int i) {
-  const int64_t most = w.tiles[i] * (((int64_t)p.table_len * p.page + kLeastChunk - 1) / kLeastChunk);
-  const int64_t chunks = 2 * (int64_t)w.deal[i].target();
+  const int64_t chunks = 2 * (int64_t)w.deal[i].target(), most = most_chunks(w, p, i);
   return ((chunks < most ? chunks : most) * p.Hkv) << w.deal[i].rows_log2;
 }
 int64_t part_bytes(const Plan& w, const Paged& p, int i) {
@@ -179,6 +187,7 @@ hipError_t launch_paged_attention(const PagedAttention& x, void* workspace, hipS
     a.causal = x.causal;
     if (w.tiles[i] == 0) continue;
     a.n_tiles = (int)w.tiles[i];
+    a.n_units = (int)units_of(w, p, i);
     if (w.deal[i].round > 0) {
       const int64_t slots = slots_of(w, p, i);
       a.part_acc = (float*)at;

@@ -134,8 +134,8 @@ struct ShareScratch {
 // There are at most target + tiles of them, and at most 2 target with more than one chunk to their tile: such a tile has
 // over chunk_keys keys, so ceil(keys / chunk_keys) is below twice keys / chunk_keys, and the sum of all keys / chunk_keys
 // is at most target.  All of this holds for sequences that do not overlap; where the arrays say nonsense and more tiles
-// come of it than the host has counted (n_tiles), the batch has no shares.  Called by whole workgroups of 256 threads.  last_first: shares of batches of up to 64 sequences
-// are numbered from the last one on.
+// come of it than the host has counted (n_tiles), the batch has no shares.  Called by whole workgroups of 256 threads.
+// last_first: shares of batches of up to 64 sequences are numbered from the last one on.
 __device__ __forceinline__ bool find_share(const Paged& p, const Deal& d, int n_tiles, int unit, ShareScratch* scratch,
                                            bool last_first, Share* out) {
   const int lane = threadIdx.x & 63;
