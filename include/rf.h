@@ -363,7 +363,8 @@ RF_API rf_status rf_paged_attention_ws(const rf_tensor* q, const rf_tensor* k_ca
  * Verification of drafted tokens against the target's probabilities, with given random numbers.  A sequence's rows
  * r = 0 .. n (packed by seq_start as above) hold the target's probabilities p_r, the draft's q_r, and x_r, the token
  * drafted from q_r; its last row has no draft:
- *   a = the first r < n with u_accept[r] q_r(x_r) >= p_r(x_r), n if there is none;  x_0 .. x_{a-1} are accepted
+ *   a = the first r < n with u_accept[r] q_r(x_r) >= p_r(x_r) (or a NaN among them), n if there is none;
+ *       x_0 .. x_{a-1} are accepted
  *   w(t) = max(0, p_a(t) - q_a(t));  where a = n, or w is 0 all over: w = max(0, p_a)
  *   the next token is the first t with w(0) + .. + w(t) > u_sample[b] sum_t w(t)
  * so that every token is distributed as the target's own would be.  Comparisons and sums are in 64 bits.
