@@ -112,8 +112,9 @@ def verify(target, draft, tokens, u_accept, u_sample, seq_start):
             if draft is not None:
                 q = draft[t0 + a].astype(np.float64)
             elif 0 <= int(tokens[t0 + a]) < len(p):
-                q[int(tokens[t0 + a])] = np.inf
-            w = np.maximum(p - q, 0)
+                q[int(tokens[t0 + a])] = 1.0
+            with np.errstate(invalid="ignore"):
+                w = np.maximum(p - q, 0)
             if w.sum() == 0:
                 w = p
         w = np.maximum(w, 0)

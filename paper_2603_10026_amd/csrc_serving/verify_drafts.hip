@@ -50,8 +50,8 @@ __device__ __forceinline__ double scan(double v) {
 
 template <typename T>
 struct Row {
-  const T *p, *q;  // q null: none, or one drafted token
-  int64_t token;   // of it (-1: none)
+  const T *p, *q;  // q null: 0, but 1 at the drafted token
+  int64_t token;   // that one (-1: none)
   int64_t V;
   // w(t) for t = t0 .. t0 + kPerVec - 1; 0 past the end
   __device__ __forceinline__ void weights(int64_t t0, double* w) const {
@@ -76,8 +76,8 @@ struct Row {
     }
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const double d = (double)a[i] - (double)b[i];
-      w[i] = d < 0 || t0 + i == token ? 0.0 : d;  // (NaN stays)
+      const double d = (double)a[i] - (double)(t0 + i == token ? 1.f : b[i]);
+      w[i] = d < 0 ? 0.0 : d;  // (NaN stays)
     }
   }
   template <int THREADS>

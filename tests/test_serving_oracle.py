@@ -92,3 +92,17 @@ def test_verify_by_hand():
     assert run([0, 1, 9], [0.1, 0.9, 0], 0.0) == ([0, 2, -1], [1])              # rest (0, 0, 0.75)
     assert run([1, 2, 9], [0.1, 0.9, 0], 0.9, None) == ([1, 1, -1], [1])        # without q: the draft leaves, (0, 0.25, -)
     assert run([0, 1, 9], [0.4, 0.4, 0], math.nan)[1] == [2]
+
+
+def test_no_draft_is_probability_one_at_the_drafted_token():
+    """Also where the target is not normalised, or not a number there."""
+    r = np.random.default_rng(6)
+    for at_x in (0.1, 0.0, 3.0, math.inf, math.nan):
+        for u in (0.5, math.nan):
+            p, x = r.random((2, 6)), np.array([4, 0])
+            p[0, 4] = at_x
+            args = x, np.array([u, 0]), np.array([0.9]), np.array([0, 2])
+            alone, given = S.verify(p, None, *args), S.verify(p, np.eye(6)[x], *args)
+            assert all(np.array_equal(a, b) for a, b in zip(alone, given))
+            if not math.isfinite(at_x) and alone[1][0] == 0:
+                assert alone[0][0] == -1
