@@ -12,7 +12,8 @@
 // What bounds it is one row of p and of q for each sequence.  A row is cut into slices: the first launch finds a
 // (every workgroup for itself: two gathered values a draft, three dependent trips to memory) and sums its slice, the
 // second finds the slice that the draw falls into and then the token inside it.  Without a workspace one workgroup goes
-// over all slices of a sequence.
+// over all slices of a sequence.  A slice is summed by 256 threads in one order in either form, so that a draw at a border,
+// which the rounding of the sums decides, gives the same token.
 #include "serving_device.h"
 
 namespace rf {
@@ -23,8 +24,7 @@ constexpr int kSumThreads = 256, kDrawThreads = 1024;
 constexpr int kSlices = 64;       // at most, of a row: a lane each
 constexpr int kMostWaves = kDrawThreads / kWave;
 
-// Sum over the workgroup's threads, in every one of them.
-template <int THREADS>
+// Sum over each kSumThreads of the workgroup's threads, in every one of them.
 __device__ __forceinline__ double group_sum(double v, double* s_red) {
 #pragma unroll
   for (int m = 1; m < 64; m <<= 1) v += __shfl_xor(v, m, 64);
@@ -32,8 +32,9 @@ __device__ __forceinline__ double group_sum(double v, double* s_red) {
   if ((threadIdx.x & 63) == 0) s_red[threadIdx.x >> 6] = v;
   __syncthreads();
   v = 0;
+  const int first = threadIdx.x / kSumThreads * (kSumThreads / kWave);
 #pragma unroll
-  for (int i = 0; i < THREADS / kWave; ++i) v += s_red[i];
+  for (int i = 0; i < kSumThreads / kWave; ++i) v += s_red[first + i];
   return v;
 }
 
@@ -80,18 +81,18 @@ struct Row {
       w[i] = d < 0 ? 0.0 : d;  // (NaN stays)
     }
   }
-  template <int THREADS>
+  // Sum of w(lo .. hi - 1), of a slice to each kSumThreads of the workgroup's threads.
   __device__ __forceinline__ double slice_sum(int64_t lo, int64_t hi, double* s_red) const {
     constexpr int N = Elem<T>::kPerVec;
     double sum = 0;
 #pragma unroll 2
-    for (int64_t t = lo + threadIdx.x * N; t < hi; t += THREADS * N) {
+    for (int64_t t = lo + threadIdx.x % kSumThreads * N; t < hi; t += kSumThreads * N) {
       double w[N];
       weights(t, w);
 #pragma unroll
       for (int i = 0; i < N; ++i) sum += w[i];
     }
-    return group_sum<THREADS>(sum, s_red);
+    return group_sum(sum, s_red);
   }
   // The first t of lo .. hi - 1 of weight above 0 whose running sum is over x; the last one of weight above 0 if none is
   // (the border was lost to the order of the sums), -1 without such a one.  By kDrawThreads threads.
@@ -225,7 +226,7 @@ __global__ __launch_bounds__(kSumThreads) void verify_sums_kernel(const VerifyDr
   if (w.n == 0) return;
   const Row<T> row = row_of<T>(a, w, false);
   const int64_t lo = s * values;
-  const double sum = row.template slice_sum<kSumThreads>(lo, min(a.V, lo + values), s_red);
+  const double sum = row.slice_sum(lo, min(a.V, lo + values), s_red);
   if (threadIdx.x == 0) {
     sums[(int64_t)b * slices + s] = sum;
     if (s == 0) reinterpret_cast<int32_t*>(sums + (int64_t)a.B * slices)[b] = w.accepted;
@@ -255,10 +256,11 @@ __global__ __launch_bounds__(kDrawThreads) void verify_draw_kernel(const VerifyD
   double upto, total;
   for (int turn = 0;; ++turn) {
     if (sums == nullptr || turn != 0) {
-      for (int s = 0; s < slices; ++s) {
+      for (int s0 = 0; s0 < slices; s0 += kDrawThreads / kSumThreads) {
+        const int s = s0 + threadIdx.x / kSumThreads;  // (past the last slice: no values)
         const int64_t lo = s * values;
-        const double v = row.template slice_sum<kDrawThreads>(lo, min(a.V, lo + values), s_red);
-        if (threadIdx.x == 0) s_sums[s] = v;
+        const double v = row.slice_sum(lo, min(a.V, lo + values), s_red);
+        if (threadIdx.x % kSumThreads == 0 && s < slices) s_sums[s] = v;
       }
       __syncthreads();
       mine = lane < slices ? s_sums[lane] : 0.0;

@@ -68,3 +68,26 @@ def test_no_draft_is_probability_one_at_the_drafted_token(rf, V, dtype):  # noqa
         for with_ws in (False, True):
             out, acc = verify(rf, (p, draft, x, ua, us, starts), with_ws)
             assert acc == accepted.tolist() and out == want.tolist(), f"draft {draft is not None}, workspace {with_ws}"
+
+
+@pytest.mark.parametrize("V", (16384, 65536))
+@pytest.mark.parametrize("dtype", (torch.float32, BF))
+def test_draws_at_a_border_are_the_same_with_and_without_a_workspace(rf, V, dtype):  # noqa: F811
+    """Rows whose second half holds the first one's weights in another order, and a draw of one half: which side of the
+    border it falls on is up to the rounding of the sums, and has to be the same in both forms."""
+    say(f"verify at borders, V={V} {dtype}")
+    r = np.random.default_rng(710)
+    B = 64
+    half = np.exp2(r.uniform(-45, 0, (B, V // 2)))
+    p = torch.from_numpy(np.concatenate((half, r.permuted(half, axis=1)), 1)).to(dtype)
+    half = p[:, :V // 2].double().numpy()
+    assert all(math.fsum(a) == math.fsum(b) for a, b in zip(half, p[:, V // 2:].double().numpy()))
+    args = (p, None, torch.zeros(B, dtype=torch.int32), torch.zeros(B), torch.full((B,), 0.5), torch.arange(B + 1, dtype=torch.int32))
+    out, acc = verify(rf, args, False)
+    got = verify(rf, args, True)
+    assert acc == got[1] == [0] * B
+    # (either neighbour of the border; weights below the rounding of the sums may lie between)
+    for b, t in enumerate(out):
+        between = p[b, t + 1:V // 2] if t < V // 2 else p[b, V // 2:t]
+        assert math.fsum(between.double().tolist()) <= V * 2.0 ** -52 * half[b].sum()
+    assert out == got[0]
