@@ -300,7 +300,7 @@ RF_API rf_status rf_rmsnorm_gemm_ws(const rf_tensor* x, const rf_tensor* g, cons
  * The three arrays are read on the device only, so a captured graph serves every batch that fits.  Whatever they say,
  * no access leaves the tensors (rows of sequences that overlap or run backwards may be left as they were).  A page
  * number outside the cache, or more keys than max_pages has room for, is answered by NaN (see the entry points).
- * T * Hq < 2^31.
+ * T * Hq < 2^31.  A batch that takes more workgroups than a launch can have (about 2^24) is RF_ERR_UNSUPPORTED.
  */
 
 /*
@@ -369,7 +369,7 @@ RF_API rf_status rf_paged_attention_ws(const rf_tensor* q, const rf_tensor* k_ca
  *   the next token is the first t with w(0) + .. + w(t) > u_sample[b] sum_t w(t)
  * so that every token is distributed as the target's own would be.  Comparisons and sums are in 64 bits.
  *   target : [R, V] f32 or bf16, rows need not be normalised.  draft : the same shape and type, or null for drafts
- *       without probabilities of their own (q = 1 at x_r).  Any row pitch and alignment.  V >= 1.
+ *       without probabilities of their own (q = 1 at x_r).  Any row pitch and alignment.  V >= 1, B < 2^22.
  *   tokens : [R] i32 (x_r; entries of last rows are not looked at; a token outside 0 .. V-1 is refused)
  *   u_accept : [R] f32, u_sample : [B] f32, uniform in [0, 1).   seq_start : [B + 1] i32
  *   out : [R] i32: the accepted tokens, the next one, then -1.   accepted : [B] i32: a (0 for a sequence without rows)

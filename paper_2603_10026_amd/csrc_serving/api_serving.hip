@@ -137,7 +137,7 @@ rf_status check_verify(const rf_tensor* target, const rf_tensor* draft, const rf
   if ((st = check_tensor(u_sample, 1, 1)) != RF_OK) return st;
   const int64_t R = target->shape[0], V = target->shape[1], B = u_sample->shape[0];
   if (V < 1) return RF_ERR_INVALID_ARG;
-  if (R >= INT32_MAX || V >= INT32_MAX || B >= INT32_MAX) return RF_ERR_UNSUPPORTED;
+  if (R >= INT32_MAX || V >= INT32_MAX || !rf::verify_drafts_fits(B)) return RF_ERR_UNSUPPORTED;
   if ((st = check_vector(tokens, RF_I32, R)) != RF_OK) return st;
   if ((st = check_vector(u_accept, RF_F32, R)) != RF_OK) return st;
   if ((st = check_vector(u_sample, RF_F32, B)) != RF_OK) return st;
@@ -209,6 +209,7 @@ rf_status rf_paged_append(const rf_tensor* q, const rf_tensor* k, const rf_tenso
     a.sin_pitch = sin->stride[0];
     a.table_rows = cos->shape[0];
   }
+  if (!rf::paged_append_fits(p)) return RF_ERR_UNSUPPORTED;
   if (empty(p)) return RF_OK;
   a.q = q->data;
   a.k = k->data;
@@ -271,7 +272,7 @@ rf_status rf_verify_drafts(const rf_tensor* target, const rf_tensor* draft, cons
 }
 
 size_t rf_verify_drafts_workspace_bytes(int64_t B, int64_t V) {
-  if (B < 1 || V < 1 || B >= INT32_MAX || V >= INT32_MAX) return 0;
+  if (B < 1 || V < 1 || V >= INT32_MAX || !rf::verify_drafts_fits(B)) return 0;
   return rf::verify_drafts_bytes(B, V);
 }
 

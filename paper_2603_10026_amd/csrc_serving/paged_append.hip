@@ -199,16 +199,24 @@ __global__ __launch_bounds__(kThreads) void paged_append_kernel(const PagedAppen
 // 32 + 2 x 8 heads: 48 tokens 4.7 / 3.6 / 9.9, 256 tokens 5.3 / 4.8 / 10.6, 1000 tokens 8.1 / 11 / 14.4, 8500 tokens
 // 42.2 / 60 / 46.0.  From 8 MiB on results are written past the caches, which would not keep them: 25000 tokens
 // 110 us (5.7 TB/s) and 122 without, 1000 tokens 8.1 and 10.1, but 256 tokens 5.1 and 4.8.
-hipError_t launch_paged_append(const PagedAppend& a, hipStream_t s) {
-  const int64_t T = a.p.T, heads = a.p.Hq + 2 * (int64_t)a.p.Hkv;
-  const int per_turn = kWave * 8 / a.p.d;
+static bool few_tokens(const Paged& p) { return p.T <= 512; }
+static int64_t append_parts(const Paged& p) {
+  const int64_t T = p.T, heads = p.Hq + 2 * (int64_t)p.Hkv;
+  const int per_turn = kWave * 8 / p.d;
   const int64_t turns = (heads + per_turn - 1) / per_turn;
-  const bool few = T <= 512;
   const int64_t least = (turns + 5) / 6, most = (turns + 2) / 3, wanted = (16384 + T - 1) / T;
-  const int64_t parts = few ? turns : wanted < least ? least : wanted < most ? wanted : most;
-  const bool past = T * heads * a.p.d * 2 >= (8 << 20);
-  const int64_t grid = (T * parts + kThreads / kWave - 1) / (kThreads / kWave);
-  if (grid > UINT32_MAX / kThreads) return hipErrorInvalidValue;
+  return few_tokens(p) ? turns : wanted < least ? least : wanted < most ? wanted : most;
+}
+static int64_t append_grid(const Paged& p) {
+  return (p.T * append_parts(p) + kThreads / kWave - 1) / (kThreads / kWave);
+}
+
+// (a grid holds less than 2^32 threads)
+bool paged_append_fits(const Paged& p) { return p.T == 0 || append_grid(p) <= UINT32_MAX / kThreads; }
+
+hipError_t launch_paged_append(const PagedAppend& a, hipStream_t s) {
+  const int64_t T = a.p.T, heads = a.p.Hq + 2 * (int64_t)a.p.Hkv, parts = append_parts(a.p), grid = append_grid(a.p);
+  const bool few = few_tokens(a.p), past = T * heads * a.p.d * 2 >= (8 << 20);
 #define RF_APPEND(DD, F8)                                                                                        \
   if (few) hipLaunchKernelGGL((paged_append_kernel<DD, F8, 1>), dim3((unsigned)grid), dim3(kThreads), 0, s, a, (int)parts, past); \
   else hipLaunchKernelGGL((paged_append_kernel<DD, F8, 3>), dim3((unsigned)grid), dim3(kThreads), 0, s, a, (int)parts, past)

@@ -31,6 +31,7 @@ struct PagedAppend {
   float eps, k_scale, v_scale;
   int rot, interleaved, fp8;
 };
+bool paged_append_fits(const Paged& p);  // whether its launch can be that large
 hipError_t launch_paged_append(const PagedAppend& a, hipStream_t s);
 
 struct PagedAttention {
@@ -57,6 +58,7 @@ struct VerifyDrafts {
   int64_t V;
   int R, B, bf16;
 };
+bool verify_drafts_fits(int64_t B);                // whether its launches can be that large
 size_t verify_drafts_bytes(int64_t B, int64_t V);  // 0 where one launch serves the call
 hipError_t launch_verify_drafts(const VerifyDrafts& a, void* workspace, hipStream_t s);
 

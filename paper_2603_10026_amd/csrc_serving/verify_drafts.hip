@@ -288,16 +288,18 @@ int num_slices(int64_t V, int64_t values) { return (int)((V + values - 1) / valu
 
 }  // namespace
 
+// (a grid holds less than 2^32 threads)
+bool verify_drafts_fits(int64_t B) { return B <= UINT32_MAX / kDrawThreads; }
+
 size_t verify_drafts_bytes(int64_t B, int64_t V) {
   const int slices = num_slices(V, slice_values(B, V, kSumThreads * 4));  // (rows of 4-byte values have as many slices or more)
-  return slices > 1 ? ((size_t)B * slices * sizeof(double) + (size_t)B * sizeof(int32_t) + 15) & ~(size_t)15 : 0;
+  return slices > 1 && B * slices <= UINT32_MAX / kSumThreads ? ((size_t)B * slices * sizeof(double) + (size_t)B * sizeof(int32_t) + 15) & ~(size_t)15 : 0;
 }
 
 hipError_t launch_verify_drafts(const VerifyDrafts& a, void* workspace, hipStream_t s) {
   const int64_t values = slice_values(a.B, a.V, kSumThreads * (a.bf16 ? 8 : 4));
   const int slices = num_slices(a.V, values);
   double* sums = slices > 1 ? (double*)workspace : nullptr;
-  if ((int64_t)a.B * slices > UINT32_MAX / kSumThreads || a.B > UINT32_MAX / kDrawThreads) return hipErrorInvalidValue;
 #define RF_VERIFY(T)                                                                                                    \
   if (sums != nullptr)                                                                                                  \
     hipLaunchKernelGGL((verify_sums_kernel<T>), dim3((unsigned)(a.B * slices)), dim3(kSumThreads), 0, s, a, sums, slices, values); \

@@ -154,3 +154,18 @@ def test_the_binding_refuses_tensors_elsewhere():
         B.rf_paged_attention(q.half(), kv, kv, i, i[:1], i[None], 2, 0.1, stream=0)
     with pytest.raises(ValueError):
         B.rf_paged_attention(q, kv, kv, i, i[:1], i[None], 2, "one", stream=0)
+
+
+def test_more_workgroups_than_a_launch_has_are_unsupported(lib):  # noqa: F811
+    """Refused on the host, like any shape that the kernels do not cover."""
+    T, n = 1 << 30, 1 << 23
+    tall = dict(T=T, Hq=1, Hkv=1, d=64)
+    assert append(lib, **tall, qn=None, kn=None) == UNS
+    assert attend(lib, **tall) == UNS and attend(lib, with_ws=True, **tall) == UNS
+    a = paged(**tall)
+    assert lib.rf_paged_attention_workspace_bytes(a["q"], a["kc"], a["pages"], 3) == 0
+    many = dict(us=_desc([n], F32), starts=_desc([n + 1], I32), acc=_desc([n], I32))
+    assert verify(lib, **many) == UNS and verify(lib, ws=(0x10000, 1 << 40), **many) == UNS
+    assert lib.rf_verify_drafts_workspace_bytes(n, 500) == lib.rf_verify_drafts_workspace_bytes(n, 131072) == 0
+    # sums of so many slices do not fit a launch: one launch serves the call
+    assert lib.rf_verify_drafts_workspace_bytes(1 << 20, 131072) == 0 < lib.rf_verify_drafts_workspace_bytes(1 << 18, 131072)
