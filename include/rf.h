@@ -286,8 +286,8 @@ RF_API rf_status rf_rmsnorm_gemm_ws(const rf_tensor* x, const rf_tensor* g, cons
  * ---- a serving step: packed sequences over a paged cache ----
  *
  * The new tokens of B sequences are packed one behind the other: [T, heads, d] tensors in which sequence b owns the
- * rows seq_start[b] .. seq_start[b+1]-1 (0 <= seq_start[0] <= .. <= seq_start[B] <= T; a sequence may have none, and
- * rows behind the last sequence are neither read nor written).  Their keys and values live in
+ * rows seq_start[b] .. seq_start[b+1]-1 (0 <= seq_start[0] <= .. <= seq_start[B] <= T; a sequence may have none; rows
+ * of no sequence are left as they are, and what they hold does not show).  Their keys and values live in
  *   k_cache, v_cache : [n_pages, page, Hkv, d], both bf16 or both FP8 E4M3, of the same shape and strides; last axis
  *       contiguous, rows 16-byte aligned, page % 16 == 0, d in {64, 128}, at most 2^26 elements from slot to slot.  Any
  *       order of the outer axes in memory.  An FP8 element stands for its value times k_scale or v_scale (finite and
@@ -300,7 +300,8 @@ RF_API rf_status rf_rmsnorm_gemm_ws(const rf_tensor* x, const rf_tensor* g, cons
  * The three arrays are read on the device only, so a captured graph serves every batch that fits.  Whatever they say,
  * no access leaves the tensors (rows of sequences that overlap or run backwards may be left as they were).  A page
  * number outside the cache, or more keys than max_pages has room for, is answered by NaN (see the entry points).
- * T * Hq < 2^31.  A batch that takes more workgroups than a launch can have (about 2^24) is RF_ERR_UNSUPPORTED.
+ * T * Hq < 2^31; of max_pages' room, 2^31 - 2^16 - 1 keys count.  A batch that takes more workgroups than a launch can have
+ * (about 2^24) is RF_ERR_UNSUPPORTED.
  */
 
 /*
@@ -328,8 +329,8 @@ RF_API rf_status rf_paged_append(const rf_tensor* q, const rf_tensor* k, const r
  * Attention of the new tokens over their sequences' caches (the cascade of rf_cascade_attention, GQA as there):
  * a single token each, a few drafted ones, or a prompt's chunk, in any mixture.
  *   q, o : [T, Hq, d] bf16, Hq % Hkv == 0.
- *   causal != 0: token i of n sees keys j <= kv_len - n + i, otherwise all keys.  A row that sees none produces zeros,
- *       and what an unseen slot holds (NaN too) does not show.
+ *   causal != 0: token i of n sees keys j <= kv_len - n + i, otherwise all keys.  A row that sees none, or whose
+ *       scores are all -inf, produces zeros, and what an unseen slot holds (NaN too) does not show.
  *   o must not overlap the inputs.
  *   max_q : tokens of the longest sequence, for the choice of kernels; results are right for any value >= 0.
  *   Rounding: probabilities to bf16 before the second product, o to bf16 at the end, everything between in fp32.  The
@@ -350,7 +351,7 @@ RF_API rf_status rf_paged_attention(const rf_tensor* q, const rf_tensor* k_cache
  *       contents need no initialisation and are undefined afterwards.  Too small or misaligned: RF_ERR_WORKSPACE.
  *       Concurrent calls must not share a workspace.
  * The size is 0 where no sequence can be long enough to be cut (the call is then rf_paged_attention) and for shapes
- * that are refused, and at most 256 MiB.
+ * that are refused, and at most 131 MiB.
  */
 RF_API size_t rf_paged_attention_workspace_bytes(const rf_tensor* q, const rf_tensor* k_cache, const rf_tensor* pages,
                                     int64_t max_q);
@@ -367,7 +368,8 @@ RF_API rf_status rf_paged_attention_ws(const rf_tensor* q, const rf_tensor* k_ca
  *       x_0 .. x_{a-1} are accepted
  *   w(t) = max(0, p_a(t) - q_a(t));  where a = n, or w is 0 all over: w = max(0, p_a)
  *   the next token is the first t with w(0) + .. + w(t) > u_sample[b] sum_t w(t)
- * so that every token is distributed as the target's own would be.  Comparisons and sums are in 64 bits.
+ * so that every token is distributed as the target's own would be.  Comparisons and sums are in 64 bits: a draw within
+ * V 2^-52 of the sum of a border between two tokens may fall on either side of it.
  *   target : [R, V] f32 or bf16, rows need not be normalised.  draft : the same shape and type, or null for drafts
  *       without probabilities of their own (q = 1 at x_r).  Any row pitch and alignment.  V >= 1, B < 2^22.
  *   tokens : [R] i32 (x_r; entries of last rows are not looked at; a token outside 0 .. V-1 is refused)

@@ -169,3 +169,16 @@ def test_more_workgroups_than_a_launch_has_are_unsupported(lib):  # noqa: F811
     assert lib.rf_verify_drafts_workspace_bytes(n, 500) == lib.rf_verify_drafts_workspace_bytes(n, 131072) == 0
     # sums of so many slices do not fit a launch: one launch serves the call
     assert lib.rf_verify_drafts_workspace_bytes(1 << 20, 131072) == 0 < lib.rf_verify_drafts_workspace_bytes(1 << 18, 131072)
+
+
+def test_workspace_of_paged_attention_is_bounded(lib):  # noqa: F811
+    """131 MiB, whatever the batch: heads, tokens, sequences and the longest of them."""
+    largest = 0
+    for d in (64, 128):
+        for group in (1, 3, 8, 16):
+            for Hkv in (1, 2, 3, 5, 8, 16, 100, 256, 512):
+                for T, Bt in ((1, 1), (8, 8), (64, 64), (300, 2), (4096, 1), (4096, 4), (16384, 100), (100000, 3)):
+                    for mq in (1, 9, 600, 1 << 20):
+                        a = paged(T=T, Bt=Bt, Hq=group * Hkv, Hkv=Hkv, d=d, n_pages=1 << 20, width=10000)
+                        largest = max(largest, lib.rf_paged_attention_workspace_bytes(a["q"], a["kc"], a["pages"], mq))
+    assert 128 << 20 < largest <= 131 << 20
