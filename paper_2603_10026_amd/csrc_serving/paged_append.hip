@@ -198,7 +198,8 @@ __global__ __launch_bounds__(kThreads) void paged_append_kernel(const PagedAppen
 // SIMD.  us, U = 3 and 2 to 4 wavefronts a token / U = 1 and one for each turn / one wavefront with U = 2, d = 128,
 // 32 + 2 x 8 heads: 48 tokens 4.7 / 3.6 / 9.9, 256 tokens 5.3 / 4.8 / 10.6, 1000 tokens 8.1 / 11 / 14.4, 8500 tokens
 // 42.2 / 60 / 46.0.  From 8 MiB on results are written past the caches, which would not keep them: 25000 tokens
-// 110 us (5.7 TB/s) and 122 without, 1000 tokens 8.1 and 10.1, but 256 tokens 5.1 and 4.8.
+// 110 us (5.7 TB/s) and 122 without, 1000 tokens 8.1 and 10.1, but 256 tokens 5.1 and 4.8.  (All bf16 caches and heads of
+// 128: where the borders lie for d = 64, whose wavefronts turn over twice the heads, and for 8 bits has not been measured.)
 static bool few_tokens(const Paged& p) { return p.T <= 512; }
 static int64_t append_parts(const Paged& p) {
   const int64_t T = p.T, heads = p.Hq + 2 * (int64_t)p.Hkv;

@@ -103,7 +103,9 @@ struct Plan {
 
 constexpr int kRoundsRows = 4, kRoundsTiles = 2, kSlackRows = 1, kSlackTiles = 7;  // see chunk_keys_of()
 
-// Two workgroups to each of the 256 compute units; one, where the two kinds share the chip.
+// Two workgroups to each of the 256 compute units; one, where the two kinds share the chip.  That is what the kernels for
+// d = 128 hold (by registers; three for 16 rows of an 8-bit cache).  Those for d = 64 hold three (tiles, and 32 rows) to
+// five (16 rows, 8 bit): what shares for so many would gain there has not been measured.
 int round_of(const Paged& p, int64_t tiles, bool alone, int rows_log2, int slack) {
   const int workgroups = alone ? 512 : 256;
   // no sequence is long enough, or there are so many workgroups that one long sequence more or less does not matter

@@ -6,7 +6,7 @@
 // which draws from the target's distribution whatever the draft's was.
 //
 // The products, the differences and the sums are taken in 64 bits: u q and p are compared exactly, and a border between
-// two tokens lies where it lies and not within an fp32 rounding of it (a vocabulary has some hundred thousand borders,
+// two tokens is off by 2^-52 of the whole and not by an fp32 rounding of it (a vocabulary has some hundred thousand borders,
 // fp32 sums that are off by 1e-7 would move one draw in a hundred).
 //
 // What bounds it is one row of p and of q for each sequence.  A row is cut into slices: the first launch finds a
